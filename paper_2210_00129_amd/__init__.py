@@ -10,6 +10,9 @@ without a GPU for the compute calls, they raise.
     X_k      = forward_cache(X, idx)                              # cache kept rows only
     dW, db, dX = backward_linear(dY, idx, X_k, W)                 # token-subset backward
     dWd, db, dX = backward_dwconv(dY, idx, X, Wd)                 # depthwise 7x7, kept outputs
+
+The steps of a language model's block (masked attention, the norms between blocks, the token table) are in lm.py and
+re-exported here.
 """
 from __future__ import annotations
 
@@ -17,6 +20,8 @@ import torch
 
 from . import _lib
 from ._lib import GatherItem, LinearLayer, SampleDesc, SbpError  # noqa: F401
+from .lm import (NORM_LAYER, NORM_RMS, backward_attention_masked, backward_embedding, backward_residual_norm,  # noqa: F401
+                 forward_attention_masked, forward_embedding, forward_residual_norm)
 
 F32, BF16 = 0, 1
 GRID_PER_CELL, GRID_SHARED, RANDOM_MASK, TEMPORAL = 0, 1, 2, 3

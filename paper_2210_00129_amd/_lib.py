@@ -34,6 +34,23 @@ class GatherItem(ctypes.Structure):
     _fields_ = [("X", c_vp), ("idx", c_vp), ("X_k", c_vp), ("M", c_i64), ("K", c_i64), ("C", c_i32), ("layout", c_i32)]
 
 
+class AttentionDesc(ctypes.Structure):
+    """Mirror of sbp_attention_desc in include/sbp_lm.h."""
+    _fields_ = [("B", c_i32), ("n", c_i32), ("h", c_i32), ("h_kv", c_i32), ("d", c_i32), ("causal", c_i32), ("scale", ctypes.c_float),
+                ("cap", ctypes.c_float), ("slopes", c_vp), ("doc", c_vp), ("prefix", c_vp)]
+
+
+class ResidualNormDesc(ctypes.Structure):
+    """Mirror of sbp_residual_norm_desc in include/sbp_lm.h."""
+    _fields_ = [("M", c_i64), ("C", c_i32), ("kind", c_i32), ("G", c_i32), ("alpha", ctypes.c_float), ("eps", ctypes.c_float),
+                ("reserved", c_u32), ("gate", c_vp), ("gamma_post", c_vp), ("beta_post", c_vp), ("gamma_pre", c_vp), ("beta_pre", c_vp)]
+
+
+class ResidualNormGrads(ctypes.Structure):
+    """Mirror of sbp_residual_norm_grads in include/sbp_lm.h."""
+    _fields_ = [("dgate", c_vp), ("dgamma_post", c_vp), ("dbeta_post", c_vp), ("dgamma_pre", c_vp), ("dbeta_pre", c_vp)]
+
+
 # name -> (restype, argtypes); every symbol include/sbp.h declares
 PROTOTYPES = {
     "sbp_status_string": (ctypes.c_char_p, [c_i32]),
@@ -75,6 +92,22 @@ PROTOTYPES = {
     "sbp_profile_read": (c_i32, [c_i32, ctypes.POINTER(c_dbl), ctypes.POINTER(c_i64)]),
 }
 
+# ... and every symbol include/sbp_lm.h declares
+LM_PROTOTYPES = {
+    "sbp_forward_attention_masked": (c_i32, [ctypes.POINTER(AttentionDesc), c_vp, c_i32, c_vp, c_vp, c_vp]),
+    "sbp_backward_attention_masked_workspace": (c_sz, [ctypes.POINTER(AttentionDesc), c_i32, c_i32]),
+    "sbp_backward_attention_masked": (c_i32, [ctypes.POINTER(AttentionDesc), c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_sz,
+                                              c_vp]),
+    "sbp_forward_residual_norm": (c_i32, [ctypes.POINTER(ResidualNormDesc), c_vp, c_vp, c_i32, c_vp, c_vp, c_vp]),
+    "sbp_backward_residual_norm_workspace": (c_sz, [ctypes.POINTER(ResidualNormDesc), c_i64, c_i32, c_u32]),
+    "sbp_backward_residual_norm": (c_i32, [ctypes.POINTER(ResidualNormDesc), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i32, c_vp, c_vp,
+                                           ctypes.POINTER(ResidualNormGrads), c_vp, c_sz, c_u32, c_vp]),
+    "sbp_forward_embedding": (c_i32, [c_vp, c_i32, c_vp, c_i64, c_i64, c_i32, ctypes.c_float, c_i32, c_vp, c_vp]),
+    "sbp_backward_embedding_workspace": (c_sz, [c_i64, c_i64, c_i64, c_i32, c_i32, c_u32]),
+    "sbp_backward_embedding": (c_i32, [c_vp, c_vp, c_i32, c_vp, c_i64, c_i64, c_i64, c_i32, ctypes.c_float, c_i32, c_vp, c_vp, c_sz, c_u32,
+                                       c_vp]),
+}
+
 _lib = None
 
 
@@ -86,7 +119,7 @@ def lib() -> ctypes.CDLL:
                 f"{LIB_PATH} is missing: build it with `python -m paper_2210_00129_amd.build` "
                 "(there is no fallback implementation)")
         handle = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in PROTOTYPES.items():
+        for name, (res, args) in (*PROTOTYPES.items(), *LM_PROTOTYPES.items()):
             fn = getattr(handle, name)
             fn.restype = res
             fn.argtypes = args

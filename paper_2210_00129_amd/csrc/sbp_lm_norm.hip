@@ -1,0 +1,458 @@
+// The step between two blocks (sbp_lm.h): norm after a block, gate, residual sum, norm before the next block; and its backward
+// on the kept rows.
+// A team of TS threads owns a row and keeps it in registers (E channels per thread), so that every tensor is read once and
+// written once; the row's sums go over the wavefront and, for teams of several wavefronts, through LDS with one barrier per round.
+// Bound: HBM.
+#include "sbp_lm_internal.h"
+#include "sbp_mfma_gemm.h"
+
+namespace sbp {
+
+template <typename T> struct LmPiece;                      // 16 bytes of a row
+template <> struct LmPiece<float> { static constexpr int N = 4; };
+template <> struct LmPiece<uint16_t> { static constexpr int N = 8; };
+
+// The channels of a thread: pieces of 16 bytes (VEC), piece i at channel (i * TS + t) * N, or single channels i * TS + t.
+template <typename T, int TS, int E, bool VEC>
+struct LmRow {
+  static constexpr int N = VEC ? LmPiece<T>::N : 1, P = E / N;
+  static_assert(E % N == 0, "whole pieces");
+  int t, C;
+  __device__ __forceinline__ int channel(int i) const { return (i / N * TS + t) * N + i % N; }
+  __device__ __forceinline__ bool valid(int i) const { return (i / N * TS + t) * N < C; }   // (VEC: C is a multiple of N)
+  __device__ __forceinline__ void load(const T* row, float (&v)[E]) const {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * TS + t) * N;
+      if constexpr (!VEC) {
+        if constexpr (sizeof(T) == 4) v[p] = c < C ? row[c] : 0.f;
+        else v[p] = c < C ? __uint_as_float((uint32_t)row[c] << 16) : 0.f;
+      } else if constexpr (sizeof(T) == 4) {
+        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < C) w = *reinterpret_cast<const float4*>(row + c);
+        v[4 * p] = w.x; v[4 * p + 1] = w.y; v[4 * p + 2] = w.z; v[4 * p + 3] = w.w;
+      } else {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (c < C) w = *reinterpret_cast<const uint4*>(row + c);
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[8 * p + 2 * e] = bf16_lo(x[e]); v[8 * p + 2 * e + 1] = bf16_hi(x[e]); }
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* row, const float (&v)[E]) const {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * TS + t) * N;
+      if (c >= C) continue;
+      if constexpr (!VEC) {
+        if constexpr (sizeof(T) == 4) row[c] = v[p];
+        else row[c] = (uint16_t)bf16_pack(v[p], v[p]);
+      } else if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(row + c) = make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
+      } else {
+        *reinterpret_cast<uint4*>(row + c) = make_uint4(bf16_pack(v[8 * p], v[8 * p + 1]), bf16_pack(v[8 * p + 2], v[8 * p + 3]),
+                                                        bf16_pack(v[8 * p + 4], v[8 * p + 5]), bf16_pack(v[8 * p + 6], v[8 * p + 7]));
+      }
+    }
+  }
+  __device__ __forceinline__ void param(const float* v, float def, float (&out)[E]) const {
+#pragma unroll
+    for (int i = 0; i < E; ++i) out[i] = v && valid(i) ? v[channel(i)] : def;
+  }
+};
+
+// Sums of R values over the team, the same in every thread of it.  `slot` alternates between two LDS areas, so that one barrier
+// per round is enough: a wavefront writes an area again only after the barrier of the round in between.
+template <int TS, int R>
+__device__ __forceinline__ void lm_team_sum(float (&v)[R], float* red, int& slot) {
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int m = 32; m; m >>= 1) v[r] += __shfl_xor(v[r], m);
+  if constexpr (TS > 64) {
+    constexpr int W = TS / 64;
+    float* at = red + slot * (4 * W);
+    slot ^= 1;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0)
+#pragma unroll
+      for (int r = 0; r < R; ++r) at[r * W + wave] = v[r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += at[r * W + w];
+      v[r] = s;
+    }
+  }
+}
+
+struct LmNormFwd {
+  const void *x, *y;
+  void *x_out, *z;
+  const float *gate, *gamma_post, *beta_post, *gamma_pre, *beta_pre;
+  long long M, rows_per_gate;
+  int C;
+  float alpha, eps;
+};
+
+// v <- normalised v (zeros past C stay whatever they are: they are never stored nor summed)
+template <typename T, int TS, int E, bool VEC, bool LAYER>
+__device__ __forceinline__ void lm_normalise(const LmRow<T, TS, E, VEC>& io, float (&v)[E], float eps, float* red, int& slot) {
+  float s[1] = {0.f};
+  const float inv = 1.f / (float)io.C;
+  if constexpr (LAYER) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) s[0] += v[i];
+    lm_team_sum<TS, 1>(s, red, slot);
+    const float mean = s[0] * inv;
+    s[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = io.valid(i) ? v[i] - mean : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < E; ++i) s[0] = fmaf(v[i], v[i], s[0]);
+  lm_team_sum<TS, 1>(s, red, slot);
+  const float r = 1.f / sqrtf(s[0] * inv + eps);
+#pragma unroll
+  for (int i = 0; i < E; ++i) v[i] *= r;
+}
+
+template <typename T, int TS, int E, bool VEC, bool LAYER>
+__global__ void __launch_bounds__(TS < 256 ? 256 : TS) residual_norm_forward_kernel(LmNormFwd a) {
+  constexpr int TEAMS = TS < 256 ? 256 / TS : 1;
+  __shared__ float red[TS > 64 ? 8 * (TS / 64) : 1];
+  int slot = 0;
+  const int team = TEAMS > 1 ? threadIdx.x / TS : 0;
+  const LmRow<T, TS, E, VEC> io{TEAMS > 1 ? (int)threadIdx.x % TS : (int)threadIdx.x, a.C};
+  float gp[E], bp[E], gn[E], bn[E];
+  io.param(a.gamma_post, 1.f, gp); io.param(a.beta_post, 0.f, bp);
+  io.param(a.gamma_pre, 1.f, gn); io.param(a.beta_pre, 0.f, bn);
+  long long group = -1;
+  float gate[E];
+  io.param(nullptr, 1.f, gate);
+  // (teams of several wavefronts: the whole workgroup is one team, so every thread meets every barrier)
+  for (long long r = (long long)blockIdx.x * TEAMS + team; r < a.M; r += (long long)gridDim.x * TEAMS) {
+    float x[E], u[E];
+    io.load((const T*)a.x + r * a.C, x);
+    if (a.y) io.load((const T*)a.y + r * a.C, u);
+    if (a.gate && r / a.rows_per_gate != group) {
+      group = r / a.rows_per_gate;
+      io.param(a.gate + group * a.C, 1.f, gate);
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] *= a.alpha;
+    if (a.y) {
+      if (a.gamma_post) {
+        lm_normalise<T, TS, E, VEC, LAYER>(io, u, a.eps, red, slot);
+#pragma unroll
+        for (int i = 0; i < E; ++i) u[i] = fmaf(u[i], gp[i], bp[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = io.valid(i) ? fmaf(gate[i], u[i], x[i]) : 0.f;
+    }
+    if (a.x_out) io.store((T*)a.x_out + r * a.C, x);
+    if (a.z) {
+      lm_normalise<T, TS, E, VEC, LAYER>(io, x, a.eps, red, slot);
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = fmaf(x[i], gn[i], bn[i]);
+      io.store((T*)a.z + r * a.C, x);
+    }
+  }
+}
+
+struct LmNormBwd {
+  const void *dx_out, *dz, *x_out, *y;
+  void *dx, *dy;
+  const int32_t *idx, *inv;
+  const float *gate, *gamma_post, *gamma_pre;
+  float* partial;                // [G][nblocks][4][C]: sums of dz xhat, dz, t yhat, t;  NULL: no parameter gradient wanted
+  long long M, K, per_group;     // kept rows per group
+  int C, nblocks, row_blocks, drop_blocks, compact;
+  float alpha, eps;
+};
+
+// Blocks 0 .. row_blocks - 1 own kept rows (block b of group g: rows b, b + nblocks, ... of the group), the others the dropped
+// rows of dx.  Per kept row, with the row's tensors in registers: the two sums each norm's backward needs come with the sums
+// of its statistics, so a layer norm takes three rounds of sums for both norms, a root-mean-square norm two.  The gate is
+// constant within a group, so the four sums over rows serve all five parameter gradients: with S1 = sum t yhat, S2 = sum t,
+// dgate = gamma S1 + beta S2, dgamma = gate S1, dbeta = gate S2.
+template <typename T, int TS, int E, bool VEC, bool LAYER>
+__global__ void __launch_bounds__(TS < 256 ? 256 : TS) residual_norm_backward_kernel(LmNormBwd a) {
+  constexpr int TEAMS = TS < 256 ? 256 / TS : 1;
+  __shared__ float red[TS > 64 ? 8 * (TS / 64) : 1];
+  int slot = 0;
+  const int team = TEAMS > 1 ? threadIdx.x / TS : 0;
+  const LmRow<T, TS, E, VEC> io{TEAMS > 1 ? (int)threadIdx.x % TS : (int)threadIdx.x, a.C};
+  const float inv_c = 1.f / (float)a.C;
+  if ((int)blockIdx.x >= a.row_blocks) {
+    for (long long r = (long long)(blockIdx.x - a.row_blocks) * TEAMS + team; r < a.M; r += (long long)a.drop_blocks * TEAMS) {
+      const int j = a.inv[r];
+      if (j >= 0 && j < a.K && a.idx[j] == r) continue;
+      float v[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = 0.f;
+      if (a.dx_out) {
+        io.load((const T*)a.dx_out + r * a.C, v);
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] *= a.alpha;
+      }
+      io.store((T*)a.dx + r * a.C, v);
+    }
+    return;
+  }
+  const int group = blockIdx.x / a.nblocks, blk = blockIdx.x % a.nblocks;
+  float gn[E], gp[E], gate[E];
+  io.param(a.gamma_pre, 0.f, gn);
+  io.param(a.gamma_post, 1.f, gp);
+  io.param(a.gate ? a.gate + (long long)group * a.C : nullptr, 1.f, gate);
+  float acc[4][E];
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int i = 0; i < E; ++i) acc[q][i] = 0.f;
+  const long long j_end = (group + 1) * a.per_group;
+  for (long long j = group * a.per_group + (long long)blk * TEAMS + team; j < j_end; j += (long long)a.nblocks * TEAMS) {
+    const long long r = a.compact || !a.idx ? j : a.idx[j];
+    float t[E], y[E], dz[E], x[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) t[i] = dz[i] = x[i] = y[i] = 0.f;
+    if (a.dx_out) io.load((const T*)a.dx_out + r * a.C, t);
+    if (a.y) io.load((const T*)a.y + j * a.C, y);
+    if (a.dz) {
+      io.load((const T*)a.dz + j * a.C, dz);
+      io.load((const T*)a.x_out + j * a.C, x);
+    }
+    float ry = 1.f;
+    if constexpr (LAYER) {
+      float s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < E; ++i) { s[0] += x[i]; s[1] += y[i]; }
+      lm_team_sum<TS, 2>(s, red, slot);
+      const float mx = s[0] * inv_c, my = a.gamma_post ? s[1] * inv_c : 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        x[i] = io.valid(i) ? x[i] - mx : 0.f;
+        y[i] = io.valid(i) ? y[i] - my : 0.f;
+      }
+    }
+    {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float g = dz[i] * gn[i];
+        s[0] = fmaf(x[i], x[i], s[0]);
+        s[1] = fmaf(y[i], y[i], s[1]);
+        s[2] = fmaf(g, x[i], s[2]);
+        if constexpr (LAYER) s[3] += g;
+      }
+      if constexpr (LAYER) {
+        lm_team_sum<TS, 4>(s, red, slot);
+      } else {
+        float s3[3] = {s[0], s[1], s[2]};
+        lm_team_sum<TS, 3>(s3, red, slot);
+        s[0] = s3[0]; s[1] = s3[1]; s[2] = s3[2];
+      }
+      const float rx = 1.f / sqrtf(s[0] * inv_c + a.eps);
+      if (a.gamma_post) ry = 1.f / sqrtf(s[1] * inv_c + a.eps);
+      const float mgx = s[2] * inv_c * rx, mg = LAYER ? s[3] * inv_c : 0.f;
+      if (a.dz) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float hat = x[i] * rx;
+          acc[0][i] = fmaf(dz[i], hat, acc[0][i]);
+          acc[1][i] += dz[i];
+          t[i] = fmaf(rx, dz[i] * gn[i] - mg - hat * mgx, t[i]);
+        }
+      }
+    }
+    if (a.dx) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = a.alpha * t[i];
+      io.store((T*)a.dx + r * a.C, x);
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      y[i] *= ry;
+      acc[2][i] = fmaf(t[i], y[i], acc[2][i]);
+      acc[3][i] += t[i];
+    }
+    if (a.dy) {
+      if (a.gamma_post) {
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          t[i] = io.valid(i) ? t[i] * gate[i] * gp[i] : 0.f;
+          s[0] = fmaf(t[i], y[i], s[0]);
+          s[1] += t[i];
+        }
+        lm_team_sum<TS, 2>(s, red, slot);
+        const float mhy = s[0] * inv_c, mh = LAYER ? s[1] * inv_c : 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) t[i] = ry * (t[i] - mh - y[i] * mhy);
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) t[i] *= gate[i];
+      }
+      io.store((T*)a.dy + j * a.C, t);
+    }
+  }
+  if (!a.partial) return;
+  // teams of one workgroup join in order through LDS
+  if constexpr (TEAMS > 1) {
+    __shared__ float join[(TEAMS - 1) * TS * E];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (team)
+#pragma unroll
+        for (int i = 0; i < E; ++i) join[((team - 1) * E + i) * TS + io.t] = acc[q][i];
+      __syncthreads();
+      if (team == 0)
+        for (int w = 0; w < TEAMS - 1; ++w)
+#pragma unroll
+          for (int i = 0; i < E; ++i) acc[q][i] += join[(w * E + i) * TS + io.t];
+      __syncthreads();
+    }
+    if (team) return;
+  }
+  float* p = a.partial + (long long)blockIdx.x * 4 * a.C;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (io.valid(i)) p[(long long)q * a.C + io.channel(i)] = acc[q][i];
+}
+
+// Sums of the partial sums in order: 64 channels per workgroup, 16 slices of the blocks.  blockIdx.y = 0: the sums over all groups;
+// blockIdx.y = 1 + g: dgate of group g.
+__global__ void __launch_bounds__(1024) residual_norm_reduce_kernel(const float* __restrict__ partial, int G, int nblocks, int C, const float* gate,
+                                                                    const float* gamma_post, const float* beta_post, sbp_residual_norm_grads g,
+                                                                    int accumulate) {
+  __shared__ float join[16][4][64];
+  const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, own = (int)blockIdx.y - 1;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c < C) {
+    const int b0 = own < 0 ? 0 : own * nblocks, b1 = own < 0 ? G * nblocks : b0 + nblocks;
+    for (int b = b0 + slice; b < b1; b += 16) {
+      const float* p = partial + (long long)b * 4 * C + c;
+      const float f = own < 0 && gate ? gate[(long long)(b / nblocks) * C + c] : 1.f;
+      s[0] += p[0];
+      s[1] += p[C];
+      s[2] = fmaf(f, p[2LL * C], s[2]);
+      s[3] = fmaf(f, p[3LL * C], s[3]);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) join[slice][q][lane] = s[q];
+  __syncthreads();
+  if (slice || c >= C) return;
+  for (int w = 1; w < 16; ++w)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) s[q] += join[w][q][lane];
+  auto put = [&](float* out, long long at, float v) { if (out) out[at] = accumulate ? out[at] + v : v; };
+  if (own < 0) {
+    put(g.dgamma_pre, c, s[0]);
+    put(g.dbeta_pre, c, s[1]);
+    put(g.dgamma_post, c, s[2]);
+    put(g.dbeta_post, c, s[3]);
+  } else {
+    put(g.dgate, (long long)own * C + c, (gamma_post ? gamma_post[c] : 1.f) * s[2] + (beta_post ? beta_post[c] : 0.f) * s[3]);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// host side: the smallest team whose registers hold the row
+// ------------------------------------------------------------------------------------------------
+static int lm_team(int C) { return C <= 512 ? 0 : C <= 1024 ? 1 : C <= 2048 ? 2 : C <= 4096 ? 3 : C <= 8192 ? 4 : 5; }
+static int lm_rows_per_block(int team) { return team < 2 ? 4 : 1; }
+
+template <typename F>
+static void lm_for_team(int team, const F& f) {
+  switch (team) {
+    case 0: f(std::integral_constant<int, 64>{}, std::integral_constant<int, 8>{}); break;
+    case 1: f(std::integral_constant<int, 64>{}, std::integral_constant<int, 16>{}); break;
+    case 2: f(std::integral_constant<int, 256>{}, std::integral_constant<int, 8>{}); break;
+    case 3: f(std::integral_constant<int, 256>{}, std::integral_constant<int, 16>{}); break;
+    case 4: f(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{}); break;
+    default: f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 16>{}); break;
+  }
+}
+static bool lm_vec(int C, int32_t dtype, uintptr_t all) { return C % (dtype == SBP_F32 ? 4 : 8) == 0 && all % 16 == 0; }
+
+template <typename T, bool LAYER>
+static void launch_norm_fwd(const LmNormFwd& a, bool vec, hipStream_t s) {
+  const int team = lm_team(a.C), rpb = lm_rows_per_block(team);
+  const unsigned blocks = (unsigned)std::min<long long>(ceil_div(a.M, rpb), 2048);
+  lm_for_team(team, [&](auto ts, auto e) {
+    constexpr int TS = decltype(ts)::value, E = decltype(e)::value;
+    const dim3 block(TS < 256 ? 256 : TS);
+    if (vec) SBP_LAUNCH(SBP_PROF_OTHER, s, (residual_norm_forward_kernel<T, TS, E, true, LAYER>), dim3(blocks), block, 0, s, a);
+    else SBP_LAUNCH(SBP_PROF_OTHER, s, (residual_norm_forward_kernel<T, TS, E, false, LAYER>), dim3(blocks), block, 0, s, a);
+  });
+}
+
+int32_t launch_forward_residual_norm(const sbp_residual_norm_desc& d, const void* x, const void* y, int32_t dtype, void* x_out, void* z,
+                                     hipStream_t s) {
+  const LmNormFwd a{x, y, x_out, z, d.gate, d.gamma_post, d.beta_post, d.gamma_pre, d.beta_pre, d.M, d.M / d.G, d.C, d.alpha, d.eps};
+  const bool vec = lm_vec(d.C, dtype, (uintptr_t)x | (uintptr_t)y | (uintptr_t)x_out | (uintptr_t)z), layer = d.kind == SBP_NORM_LAYER;
+  if (dtype == SBP_F32) { if (layer) launch_norm_fwd<float, true>(a, vec, s); else launch_norm_fwd<float, false>(a, vec, s); }
+  else { if (layer) launch_norm_fwd<uint16_t, true>(a, vec, s); else launch_norm_fwd<uint16_t, false>(a, vec, s); }
+  return check_launch("forward_residual_norm");
+}
+
+ResidualNormPlan plan_residual_norm_backward(const sbp_residual_norm_desc& a, int64_t K, int32_t dtype, uint32_t flags) {
+  ResidualNormPlan p;
+  const int rpb = lm_rows_per_block(lm_team(a.C));
+  const int64_t per = K / a.G;
+  p.nblocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(per, rpb), std::max<int64_t>(1, 512 / a.G)));
+  p.off_partial = 0;
+  p.off_inv = align_up((size_t)a.G * p.nblocks * 4 * a.C * sizeof(float), 256);
+  p.bytes = p.off_inv + (flags & SBP_FLAG_DX_COMPACT ? 0 : align_up((size_t)a.M * sizeof(int32_t), 256));
+  return p;
+}
+
+template <typename T, bool LAYER>
+static void launch_norm_bwd(const LmNormBwd& a, bool vec, hipStream_t s) {
+  const unsigned blocks = (unsigned)(a.row_blocks + a.drop_blocks);
+  if (!blocks) return;
+  lm_for_team(lm_team(a.C), [&](auto ts, auto e) {
+    constexpr int TS = decltype(ts)::value, E = decltype(e)::value;
+    const dim3 block(TS < 256 ? 256 : TS);
+    if (vec) SBP_LAUNCH(SBP_PROF_OTHER, s, (residual_norm_backward_kernel<T, TS, E, true, LAYER>), dim3(blocks), block, 0, s, a);
+    else SBP_LAUNCH(SBP_PROF_OTHER, s, (residual_norm_backward_kernel<T, TS, E, false, LAYER>), dim3(blocks), block, 0, s, a);
+  });
+}
+
+int32_t launch_backward_residual_norm(const ResidualNormPlan& p, const sbp_residual_norm_desc& d, const void* dx_out, const void* dz,
+                                      const void* x_out, const void* y, const int32_t* idx, const int32_t* inv, int64_t K, int32_t dtype,
+                                      void* dx, void* dy, const sbp_residual_norm_grads& g, void* ws, uint32_t flags, hipStream_t s) {
+  const bool compact = flags & SBP_FLAG_DX_COMPACT, wants = g.dgate || g.dgamma_post || g.dbeta_post || g.dgamma_pre || g.dbeta_pre;
+  const bool drop = dx && !compact && K < d.M && !(dx == dx_out && d.alpha == 1.f);
+  const bool rows = (dx && K > 0) || (dy && K > 0) || wants;
+  if (drop && !inv) {
+    int32_t* own = (int32_t*)((char*)ws + p.off_inv);
+    if (K > 0) launch_build_inverse(idx, K, own, s);
+    inv = own;
+  }
+  LmNormBwd a = {};
+  a.dx_out = dx_out; a.dz = K > 0 ? dz : nullptr; a.x_out = x_out; a.y = y; a.dx = dx; a.dy = dy; a.idx = idx; a.inv = inv;
+  a.gate = d.gate; a.gamma_post = d.gamma_post; a.gamma_pre = d.gamma_pre;
+  a.partial = wants ? (float*)((char*)ws + p.off_partial) : nullptr;
+  a.M = d.M; a.K = K; a.per_group = K / d.G; a.C = d.C; a.nblocks = p.nblocks;
+  a.row_blocks = rows ? d.G * p.nblocks : 0;
+  const int rpb = lm_rows_per_block(lm_team(d.C));
+  a.drop_blocks = drop ? (int)std::min<int64_t>(ceil_div(d.M, rpb), 512) : 0;
+  a.compact = compact; a.alpha = d.alpha; a.eps = d.eps;
+  const bool vec = lm_vec(d.C, dtype, (uintptr_t)dx_out | (uintptr_t)dz | (uintptr_t)x_out | (uintptr_t)y | (uintptr_t)dx | (uintptr_t)dy);
+  const bool layer = d.kind == SBP_NORM_LAYER;
+  if (dtype == SBP_F32) { if (layer) launch_norm_bwd<float, true>(a, vec, s); else launch_norm_bwd<float, false>(a, vec, s); }
+  else { if (layer) launch_norm_bwd<uint16_t, true>(a, vec, s); else launch_norm_bwd<uint16_t, false>(a, vec, s); }
+  if (wants)
+    SBP_LAUNCH(SBP_PROF_REDUCE, s, residual_norm_reduce_kernel, dim3((unsigned)ceil_div(d.C, 64), (unsigned)(1 + (g.dgate ? d.G : 0))), dim3(1024), 0, s,
+               a.partial, d.G, p.nblocks, d.C, d.gate, d.gamma_post, d.beta_post, g, flags & SBP_FLAG_ACCUMULATE_DW ? 1 : 0);
+  return check_launch("backward_residual_norm");
+}
+
+}  // namespace sbp

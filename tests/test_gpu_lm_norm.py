@@ -1,0 +1,251 @@
+"""GPU parity of the step between two blocks (norm, gate, residual sum, norm) and its backward on the kept rows.
+
+Bounds: fp32 arithmetic over C channels with sums of at most C terms, a few roundings each: (C + 64) 2^-24 of the largest value in
+the row, times the number of chained norms; bf16 outputs another 2^-8 of the value; parameter gradients sum K rows: (K + C + 64) 2^-24
+of the sum of absolute terms' largest.  A row of dx or dy is r (h - mean(h) - hat mean(h hat)): a difference of terms of the size
+r |h| |hat|, each with that relative error, so the errors are held to the terms' size where the difference is smaller (one channel
+without a mean: h - h hat^2, which cancels to eps / (x^2 + eps) of h)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2210_00129_amd as sbp
+from lm_util import DT, f64, out_step
+from oracle import lm_oracle as lm
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+
+def _close(got, ref, rel_row, step, what, terms=0.0):
+    got = f64(got)
+    assert got.shape == ref.shape and np.isfinite(got).all(), what
+    size = np.maximum(np.abs(ref).max(axis=-1, keepdims=True) if ref.ndim > 1 else np.abs(ref).max(initial=0.0), terms)
+    over = np.abs(got - ref) - (rel_row * size + step * np.abs(ref) + 1e-30)
+    assert over.size == 0 or over.max() <= 0, (what, float(over.max()), float(np.abs(got - ref).max()))
+
+
+class Norms:
+    def __init__(self, M, C, dtype, kind, post=True, pre=True, beta=True, G=1, alpha=1.0, seed=0, mean=0.0):
+        g = torch.Generator().manual_seed(seed)
+        self.M, self.C, self.dtype, self.kind, self.G, self.alpha = M, C, dtype, kind, G, float(np.float32(alpha))
+
+        def rows():
+            return (mean + torch.randn(M, C, generator=g)).to(DT[dtype])
+
+        def vec(on, at, *shape):
+            return at + 0.2 * torch.randn(*shape, C, generator=g) if on else None
+
+        self.x, self.y, self.d_out, self.dz = rows(), rows(), (rows() - mean).to(DT[dtype]), (rows() - mean).to(DT[dtype])
+        self.gate = vec(G, 0.6, G)
+        self.vectors = dict(gamma_post=vec(post, 1.0), beta_post=vec(post and beta, 0.0), gamma_pre=vec(pre, 1.0), beta_pre=vec(pre and beta, 0.0))
+        self.pre, self.post = pre, post
+
+    def kw(self, cuda, beta_pre=True):
+        d = dict(self.vectors, gate=self.gate)
+        if not beta_pre:
+            d.pop("beta_pre")
+        d = {k: None if v is None else (v.cuda() if cuda else f64(v)) for k, v in d.items()}
+        return dict(d, kind=self.kind, eps=EPS if cuda else float(np.float32(EPS)), alpha=self.alpha)
+
+
+SIZES = [(1, 1, 1), (3, 7, 0), (5, 64, 1), (12, 200, 4), (66, 512, 3), (64, 768, 1), (33, 771, 1), (40, 1024, 2), (21, 1030, 1), (18, 2048, 1),
+         (9, 2056, 3), (10, 4096, 2), (6, 5000, 1), (4, 8192, 1), (3, 8200, 1), (2, 16384, 2), (2, 16383, 1), (700, 96, 5)]
+CASES = [(s, kind, dt, i) for i, s in enumerate(SIZES) for kind in (sbp.NORM_RMS, sbp.NORM_LAYER) for dt in ("f32", "bf16")]
+
+
+def _case(size, kind, dtype, i, **kw):
+    M, C, G = size
+    kw = dict(dict(post=i % 4 != 1, pre=i % 5 != 2, beta=i % 2 == 0, G=G, alpha=[1.0, 0.7][i % 2], seed=i), **kw)
+    return Norms(M, C, dtype, kind, **kw)
+
+
+@pytest.mark.parametrize("size,kind,dtype,i", CASES)
+def test_forward(size, kind, dtype, i):
+    c = _case(size, kind, dtype, i)
+    x, z = sbp.forward_residual_norm(c.x.cuda(), c.y.cuda(), **c.kw(True))
+    rx, rz = lm.residual_norm(f64(c.x), f64(c.y), **c.kw(False))
+    rel = 2 * (c.C + 64) * 2.0 ** -24
+    _close(x, rx, rel, out_step(dtype), "x_out")
+    assert (z is None) == (rz is None)
+    if z is not None:
+        _close(z, rz, 2 * rel, out_step(dtype), "z")
+
+
+def _kept(c, share, seed=0):
+    rng = np.random.default_rng(seed)
+    G, per = max(c.G, 1), c.M // max(c.G, 1)
+    k = max(1, int(per * share))
+    return np.concatenate([g * per + np.sort(rng.choice(per, size=k, replace=False)) for g in range(G)]).astype(np.int32)
+
+
+def _backward(c, idx, inv=None, flags=0, d_out=True, **more):
+    at = torch.from_numpy(idx).long()
+    d = c.d_out if d_out else None
+    if d is not None and flags & sbp.FLAG_DX_COMPACT:
+        d = d[at].contiguous()
+    want = ["dx", "dy_k"] + ["dgate"] * (c.gate is not None) + ["dgamma_post", "dbeta_post"] * c.post + ["dgamma_pre", "dbeta_pre"] * c.pre
+    got = sbp.backward_residual_norm(None if d is None else d.cuda(), c.dz[at].cuda() if c.pre else None, c.x[at].cuda() if c.pre else None,
+                                     c.y[at].cuda(), torch.from_numpy(idx).cuda(), c.M, inv=inv, flags=flags, want=want,
+                                     **dict(c.kw(True, beta_pre=False), **more))
+    ref = lm.residual_norm_backward(f64(c.d_out) if d_out else None, f64(c.dz)[idx] if c.pre else None, f64(c.x)[idx] if c.pre else None,
+                                    f64(c.y)[idx], idx, c.M, **c.kw(False, beta_pre=False))
+    if flags & sbp.FLAG_DX_COMPACT:
+        ref["dx"], ref["terms"]["dx"] = ref["dx"][idx], ref["terms"]["dx"][idx]
+    return got, ref, want
+
+
+def _check(c, got, ref, want, K):
+    rel = 8 * (c.C + 64) * 2.0 ** -24
+    for name in want:
+        rows = name in ("dx", "dy_k")
+        # (a channel of few rows: its sum may be small beside the row's largest terms, hence the largest over all channels)
+        _close(got[name] if rows else got[name].reshape(-1), ref[name] if rows else ref[name].reshape(-1),
+               rel if rows else rel + 4 * K * 2.0 ** -24, out_step(c.dtype) if rows else 0.0, name, ref["terms"][name] if rows else 0.0)
+
+
+@pytest.mark.parametrize("size,kind,dtype,i", CASES)
+def test_backward(size, kind, dtype, i):
+    c = _case(size, kind, dtype, i)
+    idx = _kept(c, 0.5, i)
+    got, ref, want = _backward(c, idx, flags=sbp.FLAG_DX_COMPACT if i % 3 == 2 else 0)
+    _check(c, got, ref, want, len(idx))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("share", [0.01, 0.5, 1.0])
+def test_dropped_rows_pass_the_gradient_through(dtype, share):
+    c = Norms(60, 136, dtype, 0, alpha=1.0)
+    idx = _kept(c, share)
+    inv = np.full(60, -1, dtype=np.int32)
+    inv[idx] = np.arange(len(idx))
+    for given in (None, torch.from_numpy(inv).cuda()):
+        got, ref, want = _backward(c, idx, inv=given)
+        _check(c, got, ref, want, len(idx))
+        dropped = torch.from_numpy(np.setdiff1d(np.arange(60), idx))
+        assert torch.equal(got["dx"].cpu()[dropped], c.d_out[dropped])
+
+
+def test_no_incoming_stream_gradient_counts_as_zero():
+    c = Norms(40, 256, "bf16", 1)
+    got, ref, want = _backward(c, _kept(c, 0.5), d_out=False)
+    _check(c, got, ref, want, 20)
+    assert (got["dx"].cpu()[np.setdiff1d(np.arange(40), _kept(c, 0.5))].view(torch.int16) == 0).all()
+
+
+def test_no_kept_row():
+    c = Norms(10, 64, "f32", 0, alpha=0.5)
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    empty = torch.empty(0, 64, device="cuda")
+    got = sbp.backward_residual_norm(c.d_out.cuda(), empty, empty, empty, none, 10, **c.kw(True, beta_pre=False))
+    assert torch.equal(got["dx"].cpu(), 0.5 * c.d_out) and all((got[k] == 0).all() for k in got if k.startswith(("dg", "db")))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("alpha", [1.0, 0.5])
+def test_in_place(dtype, alpha):
+    c = Norms(50, 264, dtype, 1, alpha=alpha)
+    x, z = sbp.forward_residual_norm(c.x.cuda(), c.y.cuda(), **c.kw(True))
+    for which in ("x", "y"):
+        mine = dict(x=c.x.cuda(), y=c.y.cuda())
+        x2, z2 = sbp.forward_residual_norm(mine["x"], mine["y"], x_out=mine[which], **c.kw(True))
+        assert torch.equal(x, x2) and torch.equal(z, z2)
+    idx = _kept(c, 0.5)
+    want, _, names = _backward(c, idx)
+    at, d = torch.from_numpy(idx).long(), c.d_out.cuda()
+    for alias in ("y_k", "dz_k"):
+        d, ts = c.d_out.cuda(), dict(dz_k=c.dz[at].cuda(), y_k=c.y[at].cuda())
+        got = sbp.backward_residual_norm(d, ts["dz_k"], c.x[at].cuda(), ts["y_k"], torch.from_numpy(idx).cuda(), c.M, want=names, dx=d,
+                                         dy_k=ts[alias], **c.kw(True, beta_pre=False))
+        for k in names:
+            assert torch.equal(got[k], want[k]), k
+
+
+def test_accumulated_parameter_gradients():
+    c = Norms(40, 200, "f32", 1, G=2)
+    idx = _kept(c, 0.5)
+    got, _, want = _backward(c, idx)
+    grads = {k: torch.full_like(got[k], 3.0) for k in want if k not in ("dx", "dy_k")}
+    again, _, _ = _backward(c, idx, flags=sbp.FLAG_ACCUMULATE_DW, grads=grads)
+    for k in grads:
+        assert torch.equal(again[k], 3.0 + got[k]), k
+    with pytest.raises(ValueError):
+        _backward(c, idx, flags=sbp.FLAG_ACCUMULATE_DW)
+
+
+@pytest.mark.parametrize("kind", [0, 1])
+def test_rows_far_from_zero_and_rows_of_zeros(kind):
+    """A mean of 300 times the deviation: the variance must not come out of a difference of squares.  Rows of zeros stay finite."""
+    c = Norms(20, 640, "f32", kind, mean=300.0, beta=True)
+    c.x[3] = 0.0
+    c.y[3] = 0.0
+    x, z = sbp.forward_residual_norm(c.x.cuda(), c.y.cuda(), **c.kw(True))
+    rx, rz = lm.residual_norm(f64(c.x), f64(c.y), **c.kw(False))
+    # the centred values lose the steps of the mean: 301 2^-24 (C + 64) / C per unit of deviation, for both norms in a chain
+    rel = 2 * (c.C + 64) * 2.0 ** -24 + 8 * 301 * 2.0 ** -23
+    _close(x, rx, rel, 2.0 ** -24, "x_out")
+    _close(z, rz, 2 * rel, 2.0 ** -24, "z")
+
+
+def test_first_norm_of_a_network():
+    c = Norms(30, 384, "bf16", 1)
+    v = c.vectors
+    x, z = sbp.forward_residual_norm(c.x.cuda(), None, gamma_pre=v["gamma_pre"].cuda(), beta_pre=v["beta_pre"].cuda(), kind=1)
+    assert torch.equal(x.cpu(), c.x)
+    rz = lm.residual_norm(f64(c.x), None, 1, EPS, gamma_pre=f64(v["gamma_pre"]), beta_pre=f64(v["beta_pre"]))[1]
+    _close(z, rz, 4 * (384 + 64) * 2.0 ** -24, 2.0 ** -8, "z")
+
+
+def test_tensors_at_odd_addresses():
+    """Rows that start off a 16-byte border give what aligned ones give."""
+    M, C = 24, 136
+    c = Norms(M, C, "bf16", 0)
+    x, z = sbp.forward_residual_norm(c.x.cuda(), c.y.cuda(), **c.kw(True))
+    room = torch.empty(M * C + 1, dtype=torch.bfloat16, device="cuda")
+    odd = room[1:].view(M, C)
+    odd.copy_(c.x)
+    x2, z2 = sbp.forward_residual_norm(odd, c.y.cuda(), **c.kw(True))
+    assert (x.float() - x2.float()).abs().max() <= 2.0 ** -7 * x.float().abs().max() and (z.float() - z2.float()).abs().max() <= 2.0 ** -7 * z.float().abs().max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_captured_and_replayed(dtype):
+    c = Norms(96, 520, dtype, 1, G=3)
+    idx = _kept(c, 0.5)
+    at, ix = torch.from_numpy(idx).long(), torch.from_numpy(idx).cuda()
+    kw, x, y, d, dz = c.kw(True), c.x.cuda(), c.y.cuda(), c.d_out.cuda(), c.dz[at].cuda()
+    kb = {k: v for k, v in kw.items() if k != "beta_pre"}
+
+    def step():
+        x_out, z = sbp.forward_residual_norm(x, y, **kw)
+        g = sbp.backward_residual_norm(d, dz, x_out[at.cuda()], y[at.cuda()], ix, c.M, **kb)
+        return [x_out, z, *(g[k] for k in sorted(g))]
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    at = at.cuda()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in range(4):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(seed)).to(DT[dtype]))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, step()):
+            assert torch.equal(a, b)
+
+
+def test_offsets_beyond_32_bits():
+    M, C = 300000, 8192
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.zeros(M, C, dtype=torch.bfloat16, device="cuda")
+    x[-5:] = torch.randn(5, C, generator=g, device="cuda").bfloat16()
+    gamma = torch.ones(C, device="cuda")
+    out, z = sbp.forward_residual_norm(x, x, gamma_post=gamma, gamma_pre=gamma)
+    o, z5 = sbp.forward_residual_norm(x[-5:].contiguous(), x[-5:].contiguous(), gamma_post=gamma, gamma_pre=gamma)
+    assert x.numel() > 2 ** 31 and torch.equal(out[-5:], o) and torch.equal(z[-5:], z5)
+    idx = torch.arange(M - 5, M, dtype=torch.int32, device="cuda")
+    g1 = sbp.backward_residual_norm(x, z5, o, x[-5:].contiguous(), idx, M, gamma_post=gamma, gamma_pre=gamma)
+    g2 = sbp.backward_residual_norm(x[-5:].contiguous(), z5, o, x[-5:].contiguous(), None, 5, gamma_post=gamma, gamma_pre=gamma,
+                                    flags=sbp.FLAG_DX_COMPACT)
+    assert torch.equal(g1["dx"][-5:], g2["dx"]) and torch.equal(g1["dy_k"], g2["dy_k"])
+    assert (g1["dx"][:-5] == 0).all()
