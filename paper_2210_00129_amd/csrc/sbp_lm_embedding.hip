@@ -1,5 +1,6 @@
 // The token table (sbp_lm.h): scaled lookup, and the table's gradient from the kept rows, grouped by token.
 #include <algorithm>
+#include <type_traits>
 
 #include "sbp_lm_internal.h"
 #include "sbp_mfma_gemm.h"
@@ -65,21 +66,33 @@ __global__ void __launch_bounds__(256) embedding_forward_kernel(const K* __restr
 // of the whole table (dense, as the weight gradients of the other layers are); the grouping moves 8 bytes per kept row.
 //
 // Up to kEmScan kept rows one launch does it all: every wavefront owns some table rows and looks for each of them through the
-// kept tokens in LDS.  More rows are sorted by token (stable least-significant-digit radix sort of (token, row) pairs, 11 bits a
-// pass), then a wavefront sums chunks of kEmChunk sorted rows in order, and tokens that cross a chunk's border are joined from
-// partial sums in chunk order: every sum runs in the order of idx whatever the grid does.  Table rows without a token are zeroed
-// beside the sums, by a bitmap of the tokens that occur.
+// kept tokens in LDS.  More rows are sorted by token (stable least-significant-digit radix sort of (token, row) pairs): up to
+// kEmOne of them by one workgroup with the pairs in registers and LDS, all passes in one launch; more by 64 workgroups, one launch
+// per pass.  The rest of that (first) launch zeroes the table, which takes longer than the sort of one workgroup for tables of
+// about 60 MB and more.  Then a wavefront sums chunks of kEmChunk sorted rows in order and writes the rows of the tokens that
+// end there, and tokens that cross a chunk's border are joined from partial sums in chunk order: every sum runs in the order of idx
+// whatever the grid does.
 // ------------------------------------------------------------------------------------------------
-// One launch costs less than the sort's four or five, but a token that all rows share is then summed by one wavefront.
-static constexpr int kEmScan = 256, kEmChunk = 32, kEmDigit = 11, kEmBins = 1 << kEmDigit, kEmBlocks = 64;
+// One launch costs less than the sort's three, but a token that all rows share is then summed by one wavefront.
+static constexpr int kEmScan = 256, kEmOne = 16384, kEmChunk = 32, kEmBins = 2048, kEmBlocks = 64;
 
 // A lane's columns of one row: a piece of 16 bytes of the input (VEC) or one column.
 template <typename T, bool VEC>
 struct EmCols {
   static constexpr int N = VEC ? EmPiece<T>::N : 1, SLICE = 64 * N;      // columns of a lane, of a wavefront
-  static __device__ __forceinline__ void load(const T* p, float (&v)[N]) {
-    if constexpr (VEC) EmPiece<T>::load(p, v);
-    else v[0] = em_get(p);
+  using Raw = typename std::conditional<VEC, uint4, T>::type;            // as it lies in memory
+  static __device__ __forceinline__ Raw load(const T* p) { return *reinterpret_cast<const Raw*>(p); }
+  static __device__ __forceinline__ void add(const Raw& w, float (&s)[N]) {
+    if constexpr (!VEC) {
+      s[0] += em_get(&w);
+    } else {
+      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) s[e] += __uint_as_float(x[e]);
+        else { s[2 * e] += bf16_lo(x[e]); s[2 * e + 1] += bf16_hi(x[e]); }
+      }
+    }
   }
   template <typename O>
   static __device__ __forceinline__ void put(O* o, const float (&s)[N], float scale, bool add) {
@@ -131,20 +144,18 @@ __global__ void __launch_bounds__(256) embedding_scan_kernel(const T* __restrict
       for (int q = 0; any && q < kEmScan / 64; ++q) {
         unsigned long long w = hit[q];
         while (w) {                                        // U rows in flight, added in order
-          float x[U][N];
+          typename Cols::Raw x[U];
           int n = 0;
 #pragma unroll
           for (int u = 0; u < U; ++u) {
             if (!w) break;
-            Cols::load(dE + (long long)row_s[64 * q + __ffsll((long long)w) - 1] * C + c0, x[u]);
+            x[u] = Cols::load(dE + (long long)row_s[64 * q + __ffsll((long long)w) - 1] * C + c0);
             w &= w - 1;
             n = u + 1;
           }
 #pragma unroll
           for (int u = 0; u < U; ++u)
-            if (u < n)
-#pragma unroll
-              for (int e = 0; e < N; ++e) s[e] += x[u][e];
+            if (u < n) Cols::add(x[u], s);
         }
       }
       Cols::put(out + v * C + c0, s, scale, accumulate != 0);
@@ -152,135 +163,227 @@ __global__ void __launch_bounds__(256) embedding_scan_kernel(const T* __restrict
   }
 }
 
+// Zeroes a run of 16-byte pieces (and the bytes behind them), all threads of `blocks` workgroups of NT together.
+template <int NT>
+__device__ __forceinline__ void em_fill(char* out, long long bytes, int block, int blocks) {
+  const long long pieces = bytes / 16, step = (long long)blocks * NT;
+  for (long long i = (long long)block * NT + threadIdx.x; i < pieces; i += step) reinterpret_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
+  if (block == 0)
+    for (long long i = pieces * 16 + 2 * (long long)threadIdx.x; i < bytes; i += 2 * NT) *reinterpret_cast<uint16_t*>(out + i) = 0;
+}
+
 // ---- sort ----------------------------------------------------------------------------------------------------------
-// Kept row j of block b = j / per.  hist[p][b][digit]: how many elements of block b (in the order before pass p) have the digit.
+// The lanes whose element has the same digit as this lane's, among the lanes that have one.
+__device__ __forceinline__ unsigned long long em_same(uint32_t digit, bool on, int bits) {
+  unsigned long long same = __ballot(on);
+  for (int bit = 0; bit < bits; ++bit) {
+    const unsigned long long ones = __ballot(digit >> bit & 1);
+    same &= digit >> bit & 1 ? ones : ~ones;
+  }
+  return same;
+}
+
+// One workgroup of 16 wavefronts, all passes: every wavefront holds a run of the elements in registers (R rounds of 64), finds an
+// element's place among the wavefront's own, and after the counts of all wavefronts have been added up writes it to its place in LDS.
+// The other workgroups of the launch zero the table.
+template <typename K, int R>
+__global__ void __launch_bounds__(1024) embedding_sort_kernel(const K* __restrict__ tokens, const int32_t* __restrict__ idx, int compact, int Kn,
+                                                              long long V, int bits, int passes, uint32_t* __restrict__ keys_out,
+                                                              int32_t* __restrict__ rows_out, char* __restrict__ table, long long table_bytes) {
+  if (blockIdx.x) {
+    em_fill<1024>(table, table_bytes, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
+  extern __shared__ uint32_t em_lds[];
+  uint32_t *skey = em_lds, *srow = skey + R * 1024, *count = srow + R * 1024;     // [16 * 64 * R] twice, [16][256]
+  __shared__ uint32_t scan_s[4];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, first = wave * 64 * R + lane, bins = 1 << bits;
+  uint32_t key[R], row[R], at[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int j = first + 64 * r;
+    row[r] = j < Kn ? (idx ? (uint32_t)idx[j] : (uint32_t)j) : 0u;
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int j = first + 64 * r;
+    const long long tok = j < Kn ? (long long)tokens[row[r]] : V;
+    key[r] = tok >= 0 && tok < V ? (uint32_t)tok : (uint32_t)V;
+    if (compact) row[r] = (uint32_t)j;
+  }
+  for (int p = 0; p < passes; ++p) {
+    for (int i = t; i < 16 * bins; i += 1024) count[i] = 0;
+    __syncthreads();
+    uint32_t* mine = count + wave * bins;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool on = first + 64 * r < Kn;
+      const uint32_t digit = key[r] >> (p * bits) & (bins - 1);
+      const unsigned long long same = em_same(digit, on, bits);
+      const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
+      if (on) at[r] = mine[digit] + rank;
+      __builtin_amdgcn_wave_barrier();                       // (a wavefront's LDS accesses complete in order)
+      if (on && rank + 1 == (uint32_t)__popcll(same)) mine[digit] = at[r] + 1;
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    // digit t: the elements of the wavefronts before each one, then those of the digits before it
+    uint32_t total = 0, scan = 0;
+    if (t < 256) {
+      if (t < bins)
+        for (int w = 0; w < 16; ++w) {
+          const uint32_t n = count[w * bins + t];
+          count[w * bins + t] = total;
+          total += n;
+        }
+      scan = total;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const uint32_t o = __shfl_up(scan, m);
+        scan += lane >= m ? o : 0;
+      }
+      if (lane == 63) scan_s[wave] = scan;
+    }
+    __syncthreads();
+    if (t < bins) {
+      scan -= total;
+      for (int w = 0; w < wave; ++w) scan += scan_s[w];
+      for (int w = 0; w < 16; ++w) count[w * bins + t] += scan;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (first + 64 * r < Kn) {
+        const uint32_t to = at[r] + mine[key[r] >> (p * bits) & (bins - 1)];
+        skey[to] = key[r];
+        srow[to] = row[r];
+      }
+    __syncthreads();
+    if (p + 1 < passes) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (first + 64 * r < Kn) { key[r] = skey[first + 64 * r]; row[r] = srow[first + 64 * r]; }
+      __syncthreads();
+    }
+  }
+  for (int i = t; i < Kn; i += 1024) { keys_out[i] = skey[i]; rows_out[i] = (int32_t)srow[i]; }
+}
+
+// 64 workgroups: kept row j belongs to block b = j / per.  hist[p][b][digit]: how many elements of block b (in the order before pass p)
+// have the digit.  The workgroups behind the first nb zero the table.
 template <typename K>
 __global__ void __launch_bounds__(256) embedding_count_kernel(const K* __restrict__ tokens, const int32_t* __restrict__ idx, int Kn, long long V,
-                                                              int per, int passes, uint32_t* __restrict__ hist, uint32_t* __restrict__ present,
-                                                              int words) {
-  __shared__ uint32_t bins[kEmBins];
-  const int t = threadIdx.x, nb = gridDim.x;
-  for (int i = t; i < kEmBins; i += 256) bins[i] = 0;
+                                                              int per, int nb, int bits, int passes, uint32_t* __restrict__ hist,
+                                                              char* __restrict__ table, long long table_bytes) {
+  __shared__ uint32_t bins_s[kEmBins];
+  if ((int)blockIdx.x >= nb) {
+    em_fill<256>(table, table_bytes, blockIdx.x - nb, gridDim.x - nb);
+    return;
+  }
+  const int t = threadIdx.x, bins = 1 << bits;
+  for (int i = t; i < bins; i += 256) bins_s[i] = 0;
   for (int p = 1; p < passes; ++p)
-    for (int i = t; i < kEmBins; i += 256) hist[((long long)p * nb + blockIdx.x) * kEmBins + i] = 0;
-  for (int i = blockIdx.x * 256 + t; i < words; i += nb * 256) present[i] = 0;
+    for (int i = t; i < bins; i += 256) hist[((long long)p * nb + blockIdx.x) * bins + i] = 0;
   __syncthreads();
   const long long j0 = (long long)blockIdx.x * per, j1 = min(j0 + per, (long long)Kn);
   for (long long j = j0 + t; j < j1; j += 256) {
     const long long tok = em_token(tokens, idx, j);
-    atomicAdd(&bins[(tok >= 0 && tok < V ? (uint32_t)tok : (uint32_t)V) & (kEmBins - 1)], 1u);
+    atomicAdd(&bins_s[(tok >= 0 && tok < V ? (uint32_t)tok : (uint32_t)V) & (bins - 1)], 1u);
   }
   __syncthreads();
-  for (int i = t; i < kEmBins; i += 256) hist[(long long)blockIdx.x * kEmBins + i] = bins[i];
+  for (int i = t; i < bins; i += 256) hist[(long long)blockIdx.x * bins + i] = bins_s[i];
 }
 
 // One pass: a block of four wavefronts moves its run of elements, every wavefront a quarter in order.  FIRST: the elements come from
-// the tokens, and the bitmap of those that occur is made; later passes read the pairs of the pass before.
+// the tokens; later passes read the pairs of the pass before.
 template <typename K, bool FIRST>
 __global__ void __launch_bounds__(256) embedding_move_kernel(const K* __restrict__ tokens, const int32_t* __restrict__ idx, int compact,
                                                              const uint32_t* __restrict__ keys, const int32_t* __restrict__ rows, int Kn, long long V,
-                                                             int per, int pass, int passes, uint32_t* __restrict__ hist,
-                                                             uint32_t* __restrict__ present, uint32_t* __restrict__ keys_out,
-                                                             int32_t* __restrict__ rows_out) {
-  __shared__ uint32_t place[4][kEmBins];
+                                                             int per, int bits, int pass, int passes, uint32_t* __restrict__ hist,
+                                                             uint32_t* __restrict__ keys_out, int32_t* __restrict__ rows_out) {
+  __shared__ uint32_t place[4 * kEmBins];
   __shared__ uint32_t wave_total[4];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, nb = gridDim.x, shift = pass * kEmDigit;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, nb = gridDim.x, shift = pass * bits, bins = 1 << bits;
   const long long first = (long long)blockIdx.x * per + (long long)wave * (per / 4);
   const long long last = min(min(first + per / 4, (long long)(blockIdx.x + 1) * per), (long long)Kn);
-  for (int i = t; i < 4 * kEmBins; i += 256) (&place[0][0])[i] = 0;
+  uint32_t* mine = place + wave * bins;
+  for (int i = t; i < 4 * bins; i += 256) place[i] = 0;
   __syncthreads();
   auto key_at = [&](long long j) -> uint32_t {
     if constexpr (!FIRST) return keys[j];
     const long long tok = em_token(tokens, idx, j);
     return tok >= 0 && tok < V ? (uint32_t)tok : (uint32_t)V;
   };
-  for (long long j = first + lane; j < last; j += 64) atomicAdd(&place[wave][key_at(j) >> shift & (kEmBins - 1)], 1u);
-  // where the block's elements of each digit go: digits below it, then the blocks before this one
-  constexpr int PT = kEmBins / 256;
-  const uint32_t* h = hist + (long long)pass * nb * kEmBins + t * PT;
-  uint32_t total[PT], before[PT], sum = 0;
-#pragma unroll
-  for (int e = 0; e < PT; ++e) total[e] = before[e] = 0;
-  for (int b = 0; b < nb; ++b) {
-    uint32_t x[PT];
-#pragma unroll
-    for (int e = 0; e < PT; ++e) x[e] = h[(long long)b * kEmBins + e];
-#pragma unroll
-    for (int e = 0; e < PT; ++e) { before[e] += b < (int)blockIdx.x ? x[e] : 0; total[e] += x[e]; }
-  }
-#pragma unroll
-  for (int e = 0; e < PT; ++e) sum += total[e];
-  uint32_t scan = sum;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const uint32_t o = __shfl_up(scan, m);
-    scan += lane >= m ? o : 0;
-  }
-  if (lane == 63) wave_total[wave] = scan;
+  for (long long j = first + lane; j < last; j += 64) atomicAdd(&mine[key_at(j) >> shift & (bins - 1)], 1u);
   __syncthreads();
-  uint32_t at = scan - sum;
-  for (int w = 0; w < wave; ++w) at += wave_total[w];
-#pragma unroll
-  for (int e = 0; e < PT; ++e) {
-    uint32_t p = at + before[e];
-    at += total[e];
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t n = place[w][t * PT + e];
-      place[w][t * PT + e] = p;
-      p += n;
+  // where the block's elements of each digit go: the digits below it (runs of 256 digits in turn), the blocks before this one, the
+  // wavefronts before each one
+  uint32_t below = 0;
+  for (int d0 = 0; d0 < bins; d0 += 256) {
+    const int d = d0 + t;
+    uint32_t total = 0, before = 0;
+    if (d < bins) {
+      const uint32_t* h = hist + (long long)pass * nb * bins + d;
+#pragma unroll 16
+      for (int b = 0; b < nb; ++b) {
+        const uint32_t x = h[(long long)b * bins];
+        before += b < (int)blockIdx.x ? x : 0;
+        total += x;
+      }
     }
+    uint32_t scan = total;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const uint32_t o = __shfl_up(scan, m);
+      scan += lane >= m ? o : 0;
+    }
+    if (lane == 63) wave_total[wave] = scan;
+    __syncthreads();
+    uint32_t p = below + scan - total + before;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) p += wave_total[w];
+      below += wave_total[w];
+    }
+    if (d < bins)
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t n = place[w * bins + d];
+        place[w * bins + d] = p;
+        p += n;
+      }
+    __syncthreads();
   }
-  __syncthreads();
-  volatile uint32_t* mine = place[wave];
   for (long long j0 = first; j0 < last; j0 += 64) {          // (the same count for every lane)
     const long long j = j0 + lane;
     const bool on = j < last;
-    const uint32_t key = on ? key_at(j) : 0, digit = key >> shift & (kEmBins - 1);
+    const uint32_t key = on ? key_at(j) : 0, digit = key >> shift & (bins - 1);
     const int32_t row = !on ? 0 : FIRST ? (compact || !idx ? (int32_t)j : idx[j]) : rows[j];
-    unsigned long long same = __ballot(on);
-#pragma unroll
-    for (int bit = 0; bit < kEmDigit; ++bit) {
-      const unsigned long long ones = __ballot(digit >> bit & 1);
-      same &= digit >> bit & 1 ? ones : ~ones;
-    }
-    const uint32_t rank = __popcll(same & ((1ull << lane) - 1)), count = __popcll(same);
+    const unsigned long long same = em_same(digit, on, bits);
+    const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
     uint32_t dest = 0;
     if (on) dest = mine[digit] + rank;
-    if (on && rank == count - 1) mine[digit] = dest + 1;     // (a wavefront's LDS accesses complete in order)
+    __builtin_amdgcn_wave_barrier();                         // (a wavefront's LDS accesses complete in order)
+    if (on && rank + 1 == (uint32_t)__popcll(same)) mine[digit] = dest + 1;
+    __builtin_amdgcn_wave_barrier();
     if (on) {
       keys_out[dest] = key;
       rows_out[dest] = row;
-      if (FIRST && key < (uint32_t)V) atomicOr(&present[key >> 5], 1u << (key & 31));
-      if (pass + 1 < passes) atomicAdd(&hist[((long long)(pass + 1) * nb + dest / per) * kEmBins + (key >> (shift + kEmDigit) & (kEmBins - 1))], 1u);
+      if (pass + 1 < passes) atomicAdd(&hist[((long long)(pass + 1) * nb + dest / per) * bins + (key >> (shift + bits) & (bins - 1))], 1u);
     }
   }
 }
 
 // ---- sums ----------------------------------------------------------------------------------------------------------
-// Wavefronts: first (chunk, column slice) units, then runs of kEmFill table rows to be zeroed where no token occurs.  A token that lies
-// in the chunk altogether is finished here; one that began before it leaves its part in partial[chunk][0], one that begins here
-// and goes on in partial[chunk][1].
-static constexpr int kEmFill = 8;
-
+// A wavefront per (chunk, column slice).  A token that lies in the chunk altogether is finished here; one that began before it leaves
+// its part in partial[chunk][0], one that begins here and goes on in partial[chunk][1].
 template <typename T, typename O, bool VEC>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(const T* __restrict__ dE, const uint32_t* __restrict__ keys, const int32_t* __restrict__ rows,
-                                                            const uint32_t* __restrict__ present, int Kn, long long V, int C, int chunks, int slices,
-                                                            long long fills, float scale, int accumulate, float* __restrict__ partial,
-                                                            O* __restrict__ out) {
+                                                            int Kn, long long V, int C, int chunks, int slices, float scale, int accumulate,
+                                                            float* __restrict__ partial, O* __restrict__ out) {
   using Cols = EmCols<T, VEC>;
-  constexpr int N = Cols::N, U = 8;
+  constexpr int N = Cols::N, U = 16;
   const int lane = threadIdx.x & 63;
-  long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (unit >= (long long)chunks * slices) {
-    unit -= (long long)chunks * slices;
-    if (unit >= fills) return;
-    const float zero[N] = {};
-    for (long long v = unit * kEmFill; v < min((unit + 1) * kEmFill, V); ++v) {
-      if (present[v >> 5] >> (v & 31) & 1) continue;
-      for (int c = lane * N; c < C; c += Cols::SLICE) Cols::put(out + v * C + c, zero, 1.f, false);
-    }
-    return;
-  }
+  const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (unit >= (long long)chunks * slices) return;
   const int chunk = (int)(unit / slices), c0 = (int)(unit % slices) * Cols::SLICE + lane * N;
   const int i0 = chunk * kEmChunk, n = min(kEmChunk, Kn - i0);
   const bool on = c0 < C;
@@ -296,17 +399,16 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const T* __restrict_
   for (int e = 0; e < N; ++e) s[e] = 0.f;
   bool head = true;                                        // still in the chunk's first token
   for (int i = 0; i < n; i += U) {
-    float x[U][N];
+    typename Cols::Raw x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {                            // (past the chunk's end its last row again, unused)
       const long long r = __builtin_amdgcn_readlane(row, min(i + u, n - 1) + 1);
-      Cols::load(src + r * C, x[u]);
+      x[u] = Cols::load(src + r * C);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i + u >= n) break;
-#pragma unroll
-      for (int e = 0; e < N; ++e) s[e] += x[u][e];
+      Cols::add(x[u], s);
       const bool end = ends >> (i + u + 1) & 1;
       if (!end && i + u + 1 < n) continue;
       const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key, i + u + 1);
@@ -372,16 +474,22 @@ EmbeddingPlan plan_embedding_backward(int64_t K, int64_t V, int32_t C, int32_t) 
   EmbeddingPlan p = {};
   p.sorted = K > kEmScan;
   if (!p.sorted) return p;
-  p.nblocks = (int)std::min<int64_t>(kEmBlocks, ceil_div(K, 2048));
-  p.per = align_up((size_t)ceil_div(K, p.nblocks), 256);
-  p.nblocks = (int)ceil_div(K, p.per);
-  for (p.passes = 1; (V >> (p.passes * kEmDigit)) != 0; ++p.passes) {}
+  int need = 1;                                             // bits of the keys 0 .. V
+  while (V >> need) ++need;
+  if (K <= kEmOne) {
+    p.nblocks = 1;
+    p.passes = (int)ceil_div(need, 8);
+  } else {
+    p.per = align_up((size_t)ceil_div(K, kEmBlocks), 256);
+    p.nblocks = (int)ceil_div(K, p.per);
+    p.passes = (int)ceil_div(need, 11);
+  }
+  p.bits = (int)ceil_div(need, p.passes);
   p.chunks = (int)ceil_div(K, kEmChunk);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
   for (int i = 0; i < 2; ++i) { p.off_keys[i] = take(4 * K); p.off_rows[i] = take(4 * K); }
-  p.off_hist = take((size_t)p.passes * p.nblocks * kEmBins * 4);
-  p.off_present = take((size_t)ceil_div(V, 32) * 4);
+  p.off_hist = take(K <= kEmOne ? 0 : (size_t)p.passes * p.nblocks * (4 << p.bits));
   p.off_partial = take((size_t)p.chunks * 2 * C * 4);
   p.bytes = at;
   return p;
@@ -406,10 +514,10 @@ template <typename T, typename O, bool VEC>
 static void launch_em_sums(const EmbeddingPlan& p, const T* dE, const uint32_t* keys, const int32_t* rows, int64_t Kn, int64_t V, int32_t C, float scale,
                            O* out, char* ws, int accumulate, hipStream_t s) {
   const int slices = (int)ceil_div(C, EmCols<T, VEC>::SLICE);
-  const long long fills = accumulate ? 0 : ceil_div(V, kEmFill), units = (long long)p.chunks * slices;
+  const long long units = (long long)p.chunks * slices;
   float* partial = (float*)(ws + p.off_partial);
-  SBP_LAUNCH(SBP_PROF_REDUCE, s, (embedding_sum_kernel<T, O, VEC>), dim3((unsigned)ceil_div(units + fills, 4)), dim3(256), 0, s, dE, keys, rows,
-             (const uint32_t*)(ws + p.off_present), (int)Kn, (long long)V, C, p.chunks, slices, fills, scale, accumulate, partial, out);
+  SBP_LAUNCH(SBP_PROF_REDUCE, s, (embedding_sum_kernel<T, O, VEC>), dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, s, dE, keys, rows, (int)Kn, (long long)V, C,
+             p.chunks, slices, scale, accumulate, partial, out);
   if (p.chunks > 1)
     SBP_LAUNCH(SBP_PROF_REDUCE, s, (embedding_join_kernel<T, O, VEC>), dim3((unsigned)ceil_div((long long)(p.chunks - 1) * slices, 4)), dim3(256), 0, s,
                keys, partial, (int)Kn, (long long)V, C, p.chunks, slices, scale, accumulate, out);
@@ -428,17 +536,39 @@ static void launch_em_bwd(const EmbeddingPlan& p, const void* dE, const void* to
     return;
   }
   char* ws = (char*)ws_;
-  uint32_t *hist = (uint32_t*)(ws + p.off_hist), *present = (uint32_t*)(ws + p.off_present);
-  SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_count_kernel<K>), dim3(p.nblocks), dim3(256), 0, s, (const K*)tokens, idx, (int)Kn, (long long)V, (int)p.per, p.passes,
-             hist, present, (int)ceil_div(V, 32));
-  for (int q = 0; q < p.passes; ++q) {
-    uint32_t *ki = (uint32_t*)(ws + p.off_keys[(q + 1) & 1]), *ko = (uint32_t*)(ws + p.off_keys[q & 1]);
-    int32_t *ri = (int32_t*)(ws + p.off_rows[(q + 1) & 1]), *ro = (int32_t*)(ws + p.off_rows[q & 1]);
-    if (q == 0) SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_move_kernel<K, true>), dim3(p.nblocks), dim3(256), 0, s, (const K*)tokens, idx, compact, ki, ri, (int)Kn, (long long)V, (int)p.per, q, p.passes, hist, present, ko, ro);
-    else SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_move_kernel<K, false>), dim3(p.nblocks), dim3(256), 0, s, (const K*)tokens, idx, compact, ki, ri, (int)Kn, (long long)V, (int)p.per, q, p.passes, hist, present, ko, ro);
+  const long long fill = accumulate ? 0 : (long long)V * C * (long long)sizeof(O);
+  const uint32_t* keys;
+  const int32_t* rows;
+  if (Kn <= kEmOne) {
+    uint32_t* ko = (uint32_t*)(ws + p.off_keys[0]);
+    int32_t* ro = (int32_t*)(ws + p.off_rows[0]);
+    // (a filling workgroup has one piece of 16 bytes per thread at least, and the chip holds about two of these workgroups per CU)
+    const unsigned fillers = (unsigned)std::min<long long>(ceil_div(fill, 16 * 1024), 511);
+    auto go = [&](auto r) {
+      constexpr int R = decltype(r)::value;
+      const size_t lds = (size_t)(2 * R * 1024 + 16 * 256) * 4;
+      allow_dynamic_lds(reinterpret_cast<const void*>(embedding_sort_kernel<K, R>), lds);
+      SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_sort_kernel<K, R>), dim3(1 + fillers), dim3(1024), lds, s, (const K*)tokens, idx, compact, (int)Kn, (long long)V,
+                 p.bits, p.passes, ko, ro, (char*)out, fill);
+    };
+    if (Kn <= 1024) go(std::integral_constant<int, 1>{});
+    else if (Kn <= 4096) go(std::integral_constant<int, 4>{});
+    else go(std::integral_constant<int, 16>{});
+    keys = ko; rows = ro;
+  } else {
+    uint32_t* hist = (uint32_t*)(ws + p.off_hist);
+    const unsigned fillers = (unsigned)std::min<long long>(ceil_div(fill, 16 * 256), 2048);
+    SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_count_kernel<K>), dim3(p.nblocks + fillers), dim3(256), 0, s, (const K*)tokens, idx, (int)Kn, (long long)V, (int)p.per,
+               p.nblocks, p.bits, p.passes, hist, (char*)out, fill);
+    for (int q = 0; q < p.passes; ++q) {
+      uint32_t *ki = (uint32_t*)(ws + p.off_keys[(q + 1) & 1]), *ko = (uint32_t*)(ws + p.off_keys[q & 1]);
+      int32_t *ri = (int32_t*)(ws + p.off_rows[(q + 1) & 1]), *ro = (int32_t*)(ws + p.off_rows[q & 1]);
+      if (q == 0) SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_move_kernel<K, true>), dim3(p.nblocks), dim3(256), 0, s, (const K*)tokens, idx, compact, ki, ri, (int)Kn, (long long)V, (int)p.per, p.bits, q, p.passes, hist, ko, ro);
+      else SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_move_kernel<K, false>), dim3(p.nblocks), dim3(256), 0, s, (const K*)tokens, idx, compact, ki, ri, (int)Kn, (long long)V, (int)p.per, p.bits, q, p.passes, hist, ko, ro);
+    }
+    keys = (const uint32_t*)(ws + p.off_keys[(p.passes + 1) & 1]);
+    rows = (const int32_t*)(ws + p.off_rows[(p.passes + 1) & 1]);
   }
-  const uint32_t* keys = (const uint32_t*)(ws + p.off_keys[(p.passes + 1) & 1]);
-  const int32_t* rows = (const int32_t*)(ws + p.off_rows[(p.passes + 1) & 1]);
   if (vec) launch_em_sums<T, O, true>(p, (const T*)dE, keys, rows, Kn, V, C, scale, (O*)out, ws, accumulate, s);
   else launch_em_sums<T, O, false>(p, (const T*)dE, keys, rows, Kn, V, C, scale, (O*)out, ws, accumulate, s);
 }

@@ -47,9 +47,9 @@ struct EmbeddingPlan {
   bool    sorted;                // else every wavefront looks through the kept tokens for its own table rows
   int     nblocks;               // sort: workgroups, each over a run of `per` kept rows
   int64_t per;
-  int     passes;                // sort: digits of 11 bits
+  int     passes, bits;          // sort: digits and bits of one
   int     chunks;                // runs of sorted rows that one wavefront sums
-  size_t  off_keys[2], off_rows[2], off_hist, off_present, off_partial, bytes;
+  size_t  off_keys[2], off_rows[2], off_hist, off_partial, bytes;
 };
 EmbeddingPlan plan_embedding_backward(int64_t K, int64_t V, int32_t C, int32_t dtype);
 int32_t launch_forward_embedding(const void* tokens, int32_t token_bytes, const void* table, int64_t M, int64_t V, int32_t C, float scale,
