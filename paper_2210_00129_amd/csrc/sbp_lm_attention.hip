@@ -41,8 +41,12 @@ MaskedAttentionPlan plan_masked_attention_backward(const sbp_attention_desc&, in
 
 int32_t launch_forward_attention_masked(const MaskedAttention& a, int32_t dtype, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.B * a.h * ceil_div(a.rows, 32)));
-  if (dtype == SBP_BF16) SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_forward_rows_kernel<uint16_t>), grid, dim3(256), 0, s, a);
-  else SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_forward_rows_kernel<float>), grid, dim3(256), 0, s, a);
+  if (dtype == SBP_BF16) {
+    if (a.d == 16) launch_masked_forward_bf16<16>(a, s);
+    else if (a.d == 32) launch_masked_forward_bf16<32>(a, s);
+    else if (a.d == 64) launch_masked_forward_bf16<64>(a, s);
+    else launch_masked_forward_bf16<128>(a, s);
+  } else SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_forward_rows_kernel<float>), grid, dim3(256), 0, s, a);
   return check_launch("forward_attention_masked");
 }
 

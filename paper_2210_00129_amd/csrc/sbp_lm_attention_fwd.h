@@ -1,0 +1,326 @@
+// Forward of the masked attention on the bf16 matrix cores.
+//
+// A workgroup of NW wavefronts owns 32 NW queries of one (sample, query head), every wavefront 32 of them, with the q fragments, the
+// output accumulators and the softmax statistics in registers; the rows of k and v stream through LDS in tiles of 64, one pass.
+//   S^T = K Q^T: rows j, column i = lane (v_mfma_f32_32x32x16_bf16, layouts at sbp_attention.hip).  A query's scores of a block of 32
+//   keys are 16 registers in each of lanes i and i + 32, so its maximum and sum need one exchange between the halves, and P^T is,
+//   packed to bf16, the B operand of O^T += V^T P^T as it is; V^T comes out of LDS with transposing reads.
+// P is rounded to bf16 (2^-8 of the weight) because the matrix cores multiply bf16; its sum l is taken before the rounding.
+// The running maximum moves only when a block's maximum is more than kLmSlack above it (weights up to 2^kLmSlack instead of 1: no loss
+// in a floating format), so that the accumulators are rescaled rarely.
+// A stage of the loop has a product part M(t) = {O += V(t-1) P(t-1); S(t) = K(t) Q} and an arithmetic part A(t) = softmax of S(t), in
+// LDS K(t) and V(t-1).  With 8 wavefronts there are two on every SIMD, and left to themselves they do their products at the same time
+// and then their arithmetic at the same time (matrix cores busy 31 %, vector arithmetic 60 % of the cycles, next to no overlap).
+// So wavefronts 4 .. 7 run half a stage behind the others, held there by a second barrier per stage: one half's products run under
+// the other half's arithmetic.
+// Tiles that no query of the workgroup can see are never copied: with documents, a list of the others is made from the documents'
+// ranges per tile; without, they are a run of tiles.  A wavefront classes every block of 32 keys by ranges again: skipped, all
+// visible (no mask arithmetic), or masked element by element.
+// A value that is not finite in a row of v whose weight is 0 turns into NaN in the product.  Where the result of a query is not
+// finite, its row is computed again one row at a time, without the keys it does not see.
+#ifndef SBP_LM_ATTENTION_FWD_H_
+#define SBP_LM_ATTENTION_FWD_H_
+
+#include "sbp_lm_attention_tiles.h"
+
+namespace sbp {
+
+// Score arithmetic: plain (scale > 0), with the distance bias (any scale), capped with |score| <= cap <= 60 and no bias (weights
+// exp(score) themselves: no maximum is needed, exp(-60) .. exp(60) and their sums stay within fp32), capped otherwise.
+enum LmMode { LM_PLAIN = 0, LM_BIAS = 1, LM_CAP_FIXED = 2, LM_CAP = 3 };
+static constexpr float kLmSlack = 6.f, kLmFixedCap = 60.f;
+static constexpr int kLmList = 128;                        // tiles per list (8192 tokens); longer samples take several
+
+template <int D, int NW>
+struct LmFwd {
+  using L = AttnSwizzled<D>;
+  using S = LmStream<D, NW>;
+  static constexpr int STAGE = 2 * S::IMG, DOCS = 2 * STAGE;      // two stages of a k and a v tile; documents of the tokens of four k tiles
+  static constexpr int OUT = NW * 32 * (2 * D + 16);        // the output images
+  static constexpr size_t LDS = DOCS + 4 * 4 * kLmTile > OUT ? DOCS + 4 * 4 * kLmTile : OUT;
+};
+
+template <int D, int NW, int MODE>
+__global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kernel(MaskedAttention a, int nchunks) {
+  using L = AttnSwizzled<D>;
+  using F = LmFwd<D, NW>;
+  constexpr int KS = L::KS, DB = L::DB;
+  constexpr bool PAIR = NW == 8;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ int4 list_s[kLmList];                           // a tile to look at, the documents in it
+  __shared__ int range_s[2 * NW + 1];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), u = lane >> 5;
+  int rank, bh;
+  lm_unit(blockIdx.x, a.B * a.h, &rank, &bh);
+  const int chunk = a.causal ? nchunks - 1 - rank : rank;   // causal: the last queries see the most
+  const int b = bh / a.h, head = bh - b * a.h, kv = head / (a.h / a.hk), n = a.n;
+  const int ld = (a.h + 2 * a.hk) * D;
+  const uint16_t* base = (const uint16_t*)a.qkv + (long long)b * n * ld;
+  const uint16_t *k0 = base + (a.h + kv) * D, *v0 = k0 + a.hk * D;
+  const int first = chunk * 32 * NW + wave * 32, mine = first + (lane & 31), own = min(mine, n - 1);
+  const bool busy = first < n;
+  const bool docs = a.doc != nullptr;
+  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const int32_t* doc = docs ? a.doc + (long long)b * n : nullptr;
+  const int di = docs ? doc[own] : 0;
+  const L lay(lane);
+  const uint32_t lds0 = lm_lds(smem);
+  bf16x8_t qf[KS];
+  {
+    const uint16_t* q = base + (long long)own * ld + head * D + 8 * u;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(q + 16 * ks);
+  }
+  LmRange wq;                                               // of the wavefront's queries
+  wq.p0 = first; wq.p1 = min(first + 31, n - 1); wq.d0 = wq.d1 = 0;
+  if (docs) {
+    LmDocs r;
+    r.add(di);
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) r.join(m);
+    r.close();
+    wq.d0 = __builtin_amdgcn_readfirstlane(r.lo);
+    wq.d1 = __builtin_amdgcn_readfirstlane(r.hi);
+  }
+  LmRange gq;                                               // ... of the workgroup's
+  gq.p0 = chunk * 32 * NW; gq.p1 = min(gq.p0 + 32 * NW - 1, n - 1); gq.d0 = gq.d1 = 0;
+  if (docs) {
+    if (lane == 0) { range_s[wave] = wq.d0; range_s[NW + wave] = wq.d1; }
+    __syncthreads();
+    gq.d0 = range_s[0]; gq.d1 = range_s[NW];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) { gq.d0 = min(gq.d0, range_s[w]); gq.d1 = max(gq.d1, range_s[NW + w]); }
+  }
+  const float slope2 = (MODE == LM_BIAS || MODE == LM_CAP) && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+  const float c2 = a.scale * kLog2e, cap2 = a.cap * kLog2e, ct = MODE >= LM_CAP_FIXED ? 2.f * kLog2e * a.scale / a.cap : 0.f;
+
+  f32x16_t o[DB];
+#pragma unroll
+  for (int x = 0; x < DB; ++x)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[x][e] = 0.f;
+  float m2 = MODE == LM_CAP_FIXED ? 0.f : -INFINITY, l = 0.f;      // the maximum in units of log2, the half's share of the sum
+
+  f32x16_t sc[2];                                            // scores of the tile's two blocks of 32 keys
+  bf16x8_t pw[2][2];                                         // their weights
+  auto scores = [&](const char* tk) {
+    const f32x16_t zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        sc[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.row(tk, 32 * y, ks), qf[ks], ks ? sc[y] : zero, 0, 0, 0);
+  };
+  auto products = [&](const char* tv) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int x = 0; x < DB; ++x) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.tr(tv, 32 * y + 16 * ks, x), pw[y][ks], o[x], 0, 0, 0);
+  };
+  // scores of the tile at position p into weights; td: the documents of its keys
+  auto weigh = [&](bool masked, const int* td, int p) {
+    const int rel = mine - p - 4 * u;                        // distance to the lane's key of register 0
+    const float relf = (float)rel;
+    if constexpr (MODE != LM_PLAIN) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float v = sc[y][e];
+          if constexpr (MODE == LM_BIAS) v *= c2;
+          else v = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(v * ct) + 1.f), cap2);   // cap tanh(z / cap)
+          if constexpr (MODE != LM_CAP_FIXED) v = fmaf(-slope2, fabsf(relf - (float)(32 * y + 8 * (e >> 2) + (e & 3))), v);
+          sc[y][e] = v;
+        }
+    }
+    if (masked) {
+      // the lane's keys of registers with row < lim are seen: up to the query's own position or the end of the prefix, and of the sample
+      int lim = n - p - 4 * u;
+      if (a.causal) lim = min(lim, max(rel + 1, prefix - p - 4 * u));
+      if (docs && di < 0) lim = 0;
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          int4 dj = make_int4(0, 0, 0, 0);
+          if (docs) dj = *reinterpret_cast<const int4*>(td + 32 * y + 4 * u + 8 * q4);
+          const int dk[4] = {dj.x, dj.y, dj.z, dj.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool see = 32 * y + 8 * q4 + e < lim && (!docs || dk[e] == di);
+            sc[y][4 * q4 + e] = see ? sc[y][4 * q4 + e] : -INFINITY;
+          }
+        }
+    }
+    if constexpr (MODE != LM_CAP_FIXED) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) mx = fmaxf(mx, fmaxf(sc[y][e], sc[y][e + 1]));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      if constexpr (MODE == LM_PLAIN) mx *= c2;
+      if (__ballot(mx > m2 + kLmSlack)) {
+        const float mn = mx > m2 + kLmSlack ? mx : m2, f = mn > m2 ? __builtin_amdgcn_exp2f(m2 - mn) : 1.f;
+        m2 = mn;
+        l *= f;
+#pragma unroll
+        for (int x = 0; x < DB; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[x][e] *= f;
+      }
+    }
+    const float ms = m2 == -INFINITY ? 0.f : m2;             // (nothing seen so far: every weight is 0)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if constexpr (MODE == LM_PLAIN) sc[y][e] = __builtin_amdgcn_exp2f(fmaf(sc[y][e], c2, -ms));
+        else if constexpr (MODE == LM_CAP_FIXED) sc[y][e] = __builtin_amdgcn_exp2f(sc[y][e]);
+        else sc[y][e] = __builtin_amdgcn_exp2f(sc[y][e] - ms);
+        l += sc[y][e];
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) pw[y][ks] = pack8(sc[y], ks);
+    }
+  };
+
+  const int ntiles = (n + kLmTile - 1) / kLmTile;
+  const int reach = a.causal ? min(ntiles, max(gq.p1 / kLmTile + 1, (min(prefix, n) + kLmTile - 1) / kLmTile)) : ntiles;
+  for (int base_tile = 0; base_tile < reach; base_tile += kLmList) {
+    const int here = min(kLmList, reach - base_tile);
+    int ns = here;
+    if (docs) {
+      // document ranges of the tiles, four lanes to a tile, and the list of those to look at
+      __syncthreads();
+      for (int i0 = 0; i0 < here; i0 += 4 * NW) {            // 16 lanes to a tile, 4 tokens to a lane
+        const int i = i0 + (t >> 4), at = (base_tile + i) * kLmTile + (t & 15) * 4;
+        LmDocs r;
+        if (i < here) {
+          int v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = doc[min(at + e, n - 1)];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r.add(v[e]);
+        }
+#pragma unroll
+        for (int m = 1; m < 16; m <<= 1) r.join(m);
+        r.close();
+        if (i < here && (t & 15) == 0) list_s[i] = make_int4(i, r.lo, r.hi, 0);
+      }
+      __syncthreads();
+      if (wave == 0) {
+        int count = 0;
+        for (int i0 = 0; i0 < here; i0 += 64) {
+          const int i = i0 + lane, p = (base_tile + i) * kLmTile;
+          const int4 e = i < here ? list_s[i] : make_int4(0, 0, 0, 0);
+          const bool on = i < here && lm_class(gq, LmRange{p, p + kLmTile - 1, e.y, e.z}, a.causal, prefix, true) != 0;
+          const unsigned long long w = __ballot(on);
+          if (on) list_s[count + __popcll(w & ((1ull << lane) - 1))] = e;      // (in place: no entry moves up past one not yet read)
+          count += __popcll(w);
+        }
+        if (lane == 0) range_s[2 * NW] = count;
+      }
+      __syncthreads();
+      ns = __builtin_amdgcn_readfirstlane(range_s[2 * NW]);
+    }
+    auto entry = [&](int s) { return docs ? list_s[min(s, kLmList - 1)] : make_int4(s, 0, 0, 0); };
+    // copies of stage s: the k tile of entry s, the v tile of the entry before it
+    auto issue = [&](int s, int tile, int before) {
+      const uint32_t buf = lds0 + (s & 1) * F::STAGE;
+      if (s < ns) {
+        const int t0 = (base_tile + tile) * kLmTile;
+        F::S::issue_one(k0, ld, t0, n, buf, lane, wave);
+        if (docs && wave == s % NW) lm_copy4(doc + min(t0 + lane, n - 1), lds0 + F::DOCS + (s & 3) * (4 * kLmTile));
+      }
+      if (s > 0 && s <= ns) F::S::issue_one(v0, ld, (base_tile + before) * kLmTile, n, buf + F::S::IMG, lane, wave);
+    };
+        int4 mine_at = entry(0);                                 // the entry whose scores come next
+    int copied = __builtin_amdgcn_readfirstlane(mine_at.x), coming = __builtin_amdgcn_readfirstlane(entry(1).x);
+    issue(0, copied, 0);
+    const bool late = PAIR && wave >= NW / 2;                // this wavefront runs half a stage behind
+    // the meeting before stage s: its copies have arrived everywhere, the places of stage s - 1 are free; and the one half a stage later
+    auto meet = [&](bool first_half, int s) {
+      if (first_half) lm_copies_done();
+      lds_barrier();
+      if (first_half) {
+        issue(s + 1, coming, copied);
+        copied = coming;
+        coming = __builtin_amdgcn_readfirstlane(entry(s + 2).x);
+      }
+    };
+    wait_async_copies<0>();                                  // (the queries' loads too, lest the loop waits for them)
+    if (late) meet(true, 0);
+    int live = 0;                                            // 1: the tile whose scores are in sc is seen; 2: with masks
+    for (int t = 0; t <= ns; ++t) {
+      if (!late) meet(true, t);
+      else meet(false, t);
+      const char* buf = smem + (t & 1) * F::STAGE;
+      if (live) products(buf + F::S::IMG);
+      live = 0;
+      int p0 = 0;
+      if (t < ns) {
+        LmRange r;
+        p0 = (base_tile + __builtin_amdgcn_readfirstlane(mine_at.x)) * kLmTile;
+        r.p0 = p0; r.p1 = p0 + kLmTile - 1;
+        r.d0 = __builtin_amdgcn_readfirstlane(mine_at.y);
+        r.d1 = __builtin_amdgcn_readfirstlane(mine_at.z);
+        const int cls = busy ? lm_class(wq, r, a.causal, prefix, docs) : 0;
+        live = cls == 0 ? 0 : cls == 2 && r.p1 < n ? 1 : 2;
+        mine_at = entry(t + 1);
+      }
+      if (live) scores(buf);
+      if (late) meet(true, t + 1);
+      else if (PAIR) meet(false, t);
+      if (live) weigh(live == 2, reinterpret_cast<const int*>(smem + F::DOCS + (t & 3) * (4 * kLmTile)), p0);
+    }
+    if (PAIR && !late) meet(false, 0);
+    lds_barrier();                                           // the tiles have been consumed: their places are free for the next list or the output
+  }
+  if (!busy) return;
+  l += __shfl_xor(l, 32);
+  const bool empty = l == 0.f;
+  const float f = empty ? 0.f : 1.f / l;
+  bool fine = lm_finite(l);
+#pragma unroll
+  for (int x = 0; x < DB; ++x)
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (D >= 32 || e < 8) fine = fine && lm_finite(o[x][e]);
+  uint16_t* out = (uint16_t*)a.out + (long long)b * n * (a.h * D) + head * D;
+  attn_store_rows<D>(smem + wave * (32 * (2 * D + 16)), o, f, out, (long long)a.h * D, first, n, lane);
+  if (a.lse_out && u == 0 && mine < n)
+    a.lse_out[((long long)b * n + mine) * a.h + head] = empty ? -INFINITY : (m2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  unsigned long long again = __ballot(!fine);
+  again = (again | again >> 32) & 0xffffffffull;
+  for (; again; again &= again - 1) {
+    const int q = first + __ffsll((long long)again) - 1;
+    if (q < n) lm_forward_row<uint16_t>(a, b, head, q, lane);
+  }
+}
+
+template <int D, int NW, int MODE>
+static void launch_masked_forward(const MaskedAttention& a, hipStream_t s) {
+  const int nchunks = (int)ceil_div(a.n, 32 * NW);
+  constexpr size_t lds = LmFwd<D, NW>::LDS;
+  allow_dynamic_lds(reinterpret_cast<const void*>(masked_forward_kernel<D, NW, MODE>), lds);
+  SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_forward_kernel<D, NW, MODE>), dim3((unsigned)((int64_t)a.B * a.h * nchunks)), dim3(64 * NW), lds, s, a, nchunks);
+}
+template <int D, int NW>
+static void launch_masked_forward_mode(const MaskedAttention& a, hipStream_t s) {
+  const bool bias = a.slopes != nullptr;
+  if (a.cap > 0.f && !bias && a.cap <= kLmFixedCap) launch_masked_forward<D, NW, LM_CAP_FIXED>(a, s);
+  else if (a.cap > 0.f) launch_masked_forward<D, NW, LM_CAP>(a, s);
+  else if (bias || !(a.scale > 0.f)) launch_masked_forward<D, NW, LM_BIAS>(a, s);
+  else launch_masked_forward<D, NW, LM_PLAIN>(a, s);
+}
+template <int D>
+void launch_masked_forward_bf16(const MaskedAttention& a, hipStream_t s) {
+  if (a.n > (D == 128 ? 128 : 1 << 30)) launch_masked_forward_mode<D, 8>(a, s);
+  else launch_masked_forward_mode<D, 4>(a, s);
+}
+
+}  // namespace sbp
+#endif

@@ -25,6 +25,7 @@ struct MaskedAttentionPlan {     // workspace of the backward
   size_t bytes;
 };
 MaskedAttentionPlan plan_masked_attention_backward(const sbp_attention_desc& a, int32_t n_k, int32_t dtype);
+template <int D> void launch_masked_forward_bf16(const MaskedAttention& a, hipStream_t s);
 int32_t launch_forward_attention_masked(const MaskedAttention& a, int32_t dtype, hipStream_t s);
 int32_t launch_backward_attention_masked(const MaskedAttention& a, const MaskedAttentionPlan& p, int32_t dtype, void* ws, hipStream_t s);
 

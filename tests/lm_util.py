@@ -101,8 +101,9 @@ def check_forward(case, out=None):
     return A, lse
 
 
-def check_backward(case, keep=None, tensors=None, call=None):
-    """Runs the backward on the kept positions keep [B, n_k] (None: all) after the oracle's forward; returns dqkv on the GPU."""
+def check_backward(case, keep=None, run=None):
+    """Runs the backward on the kept positions keep [B, n_k] (None: all) after the oracle's forward; returns dqkv on the GPU.
+    run(qkv_k, A_k, dA_k, lse_k, idx): another call in the place of the plain one."""
     B, n, h, hk, d = case.B, case.n, case.h, case.hk, case.d
     all_kept = keep is None
     keep = np.tile(np.arange(n), (B, 1)) if all_kept else np.asarray(keep)
@@ -118,7 +119,8 @@ def check_backward(case, keep=None, tensors=None, call=None):
     qkv_k, dA_k = case.qkv[at].contiguous(), case.dA[at].contiguous()
     A_k, lse_k = torch.from_numpy(A)[at].to(DT[case.dtype]), torch.from_numpy(lse)[at].float()
     idx = None if all_kept else torch.from_numpy(rows.astype(np.int32)).cuda()
-    out = sbp.backward_attention_masked(qkv_k.cuda(), A_k.cuda(), dA_k.cuda(), lse_k.cuda(), n=n, idx=idx, **case.kw())
+    ins = (qkv_k.cuda(), A_k.cuda(), dA_k.cuda(), lse_k.cuda())
+    out = sbp.backward_attention_masked(*ins, n=n, idx=idx, **case.kw()) if run is None else run(*ins, idx)
     got = f64(out).reshape(B, nk, h + 2 * hk, d)
     step, bf = out_step(case.dtype), 2.0 ** -8 if case.dtype == "bf16" else 0.0
     for b in range(B):
