@@ -14,8 +14,8 @@
 // So wavefronts 4 .. 7 run half a stage behind the others, held there by a second barrier per stage: one half's products run under
 // the other half's arithmetic.
 // Tiles that no query of the workgroup can see are never copied: with documents, a list of the others is made from the documents'
-// ranges per tile; without, they are a run of tiles.  A wavefront classes every block of 32 keys by ranges again: skipped, all
-// visible (no mask arithmetic), or masked element by element.
+// ranges per tile; without, they are a run of tiles.  A wavefront works from the first to the last of them that it sees itself, and
+// masks element by element only where a tile is not visible altogether.
 // A value that is not finite in a row of v whose weight is 0 turns into NaN in the product.  Where the result of a query is not
 // finite, its row is computed again one row at a time, without the keys it does not see.
 #ifndef SBP_LM_ATTENTION_FWD_H_
@@ -29,6 +29,7 @@ namespace sbp {
 // exp(score) themselves: no maximum is needed, exp(-60) .. exp(60) and their sums stay within fp32), capped otherwise.
 enum LmMode { LM_PLAIN = 0, LM_BIAS = 1, LM_CAP_FIXED = 2, LM_CAP = 3 };
 static constexpr float kLmSlack = 6.f, kLmFixedCap = 60.f;
+static constexpr int kLmAhead = 6;
 static constexpr int kLmList = 128;                        // tiles per list (8192 tokens); longer samples take several
 
 template <int D, int NW>
@@ -103,22 +104,32 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
 
   f32x16_t sc[2];                                            // scores of the tile's two blocks of 32 keys
   bf16x8_t pw[2][2];                                         // their weights
-  auto scores = [&](const char* tk) {
+  // M(t): the products of a stage, P V of one tile and K Q of the next (either may be left out), with every operand read kLmAhead
+  // products before it is multiplied (the compiler by itself reads it right before, or two products ahead: a product takes 32 cycles, a
+  // read under way some 150).
+  auto multiply = [&](auto pv_, auto kq_, const char* tv, const char* tk) {
+    constexpr int NP = decltype(pv_)::value ? 4 * DB : 0, N = NP + (decltype(kq_)::value ? 2 * KS : 0), AHEAD = kLmAhead < N ? kLmAhead : N;
     const f32x16_t zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto operand = [&](int i) { return i < NP ? lay.tr(tv, 16 * (i / DB), i % DB) : lay.row(tk, 32 * ((i - NP) & 1), (i - NP) >> 1); };
+    bf16x8_t f[AHEAD];
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int i = 0; i < AHEAD; ++i) f[i] = operand(i);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        sc[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.row(tk, 32 * y, ks), qf[ks], ks ? sc[y] : zero, 0, 0, 0);
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < NP) {
+        const int g = i / DB, x = i % DB;
+        o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], pw[g >> 1][g & 1], o[x], 0, 0, 0);
+      } else {
+        const int y = (i - NP) & 1, ks = (i - NP) >> 1;
+        sc[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], qf[ks], ks ? sc[y] : zero, 0, 0, 0);
+      }
+      if (i + AHEAD < N) f[i % AHEAD] = operand(i + AHEAD);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
-  auto products = [&](const char* tv) {
-#pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int x = 0; x < DB; ++x) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.tr(tv, 32 * y + 16 * ks, x), pw[y][ks], o[x], 0, 0, 0);
-  };
+  using Yes = std::true_type;
+  using No = std::false_type;
   // scores of the tile at position p into weights; td: the documents of its keys
   auto weigh = [&](bool masked, const int* td, int p) {
     const int rel = mine - p - 4 * u;                        // distance to the lane's key of register 0
@@ -237,8 +248,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
       }
       if (s > 0 && s <= ns) F::S::issue_one(v0, ld, (base_tile + before) * kLmTile, n, buf + F::S::IMG, lane, wave);
     };
-        int4 mine_at = entry(0);                                 // the entry whose scores come next
-    int copied = __builtin_amdgcn_readfirstlane(mine_at.x), coming = __builtin_amdgcn_readfirstlane(entry(1).x);
+        int copied = __builtin_amdgcn_readfirstlane(entry(0).x), coming = __builtin_amdgcn_readfirstlane(entry(1).x);
     issue(0, copied, 0);
     const bool late = PAIR && wave >= NW / 2;                // this wavefront runs half a stage behind
     // the meeting before stage s: its copies have arrived everywhere, the places of stage s - 1 are free; and the one half a stage later
@@ -251,30 +261,58 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
         coming = __builtin_amdgcn_readfirstlane(entry(s + 2).x);
       }
     };
+    auto top = [&](int t) { meet(!late, t); };
+    auto mid = [&](int t) { if (PAIR) meet(late, t + 1); };
+    auto idle = [&](int from, int to) {
+#pragma unroll 1
+      for (int t = from; t < to; ++t) { top(t); mid(t); }
+    };
+    // the entries s0 .. s1 - 1 hold all that the wavefront sees
+    int s0 = 0, s1 = busy ? ns : 0;
+    if (docs) {
+      s0 = ns; s1 = 0;
+      for (int i0 = 0; busy && i0 < ns; i0 += 64) {
+        const int4 e = list_s[min(i0 + lane, kLmList - 1)];
+        const int p = (base_tile + e.x) * kLmTile;
+        const unsigned long long w = __ballot(i0 + lane < ns && lm_class(wq, LmRange{p, p + kLmTile - 1, e.y, e.z}, a.causal, prefix, true) != 0);
+        if (w) {
+          s0 = min(s0, i0 + __ffsll((long long)w) - 1);
+          s1 = i0 + 64 - __clzll((long long)w);
+        }
+      }
+    } else if (a.causal && busy) {
+      s1 = min(ns, max(max(wq.p1 / kLmTile + 1, (min(prefix, n) + kLmTile - 1) / kLmTile) - base_tile, 0));
+    }
+    auto stage_at = [&](int t) { return smem + (t & 1) * F::STAGE; };
+    auto weights_of = [&](int t) {
+      const int4 e = entry(t);
+      LmRange r;
+      r.p0 = (base_tile + __builtin_amdgcn_readfirstlane(e.x)) * kLmTile; r.p1 = r.p0 + kLmTile - 1;
+      r.d0 = __builtin_amdgcn_readfirstlane(e.y); r.d1 = __builtin_amdgcn_readfirstlane(e.z);
+      const bool masked = r.p1 >= n || lm_class(wq, r, a.causal, prefix, docs) != 2;
+      weigh(masked, reinterpret_cast<const int*>(smem + F::DOCS + (t & 3) * (4 * kLmTile)), r.p0);
+    };
     wait_async_copies<0>();                                  // (the queries' loads too, lest the loop waits for them)
     if (late) meet(true, 0);
-    int live = 0;                                            // 1: the tile whose scores are in sc is seen; 2: with masks
-    for (int t = 0; t <= ns; ++t) {
-      if (!late) meet(true, t);
-      else meet(false, t);
-      const char* buf = smem + (t & 1) * F::STAGE;
-      if (live) products(buf + F::S::IMG);
-      live = 0;
-      int p0 = 0;
-      if (t < ns) {
-        LmRange r;
-        p0 = (base_tile + __builtin_amdgcn_readfirstlane(mine_at.x)) * kLmTile;
-        r.p0 = p0; r.p1 = p0 + kLmTile - 1;
-        r.d0 = __builtin_amdgcn_readfirstlane(mine_at.y);
-        r.d1 = __builtin_amdgcn_readfirstlane(mine_at.z);
-        const int cls = busy ? lm_class(wq, r, a.causal, prefix, docs) : 0;
-        live = cls == 0 ? 0 : cls == 2 && r.p1 < n ? 1 : 2;
-        mine_at = entry(t + 1);
+    if (s0 < s1) {
+      idle(0, s0);
+      top(s0);
+      multiply(No{}, Yes{}, nullptr, stage_at(s0));
+      mid(s0);
+      weights_of(s0);
+#pragma unroll 1
+      for (int t = s0 + 1; t < s1; ++t) {
+        top(t);
+        multiply(Yes{}, Yes{}, stage_at(t) + F::S::IMG, stage_at(t));
+        mid(t);
+        weights_of(t);
       }
-      if (live) scores(buf);
-      if (late) meet(true, t + 1);
-      else if (PAIR) meet(false, t);
-      if (live) weigh(live == 2, reinterpret_cast<const int*>(smem + F::DOCS + (t & 3) * (4 * kLmTile)), p0);
+      top(s1);
+      multiply(Yes{}, No{}, stage_at(s1) + F::S::IMG, nullptr);
+      mid(s1);
+      idle(s1 + 1, ns + 1);
+    } else {
+      idle(0, ns + 1);
     }
     if (PAIR && !late) meet(false, 0);
     lds_barrier();                                           // the tiles have been consumed: their places are free for the next list or the output
