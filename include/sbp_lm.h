@@ -37,7 +37,7 @@ extern "C" {
  */
 typedef struct sbp_attention_desc {
   int32_t  B;             /* samples, >= 1 */
-  int32_t  n;             /* tokens per sample, >= 1 */
+  int32_t  n;             /* tokens per sample, 1 .. 2^24 */
   int32_t  h, h_kv;       /* query heads and key / value heads, h a multiple of h_kv */
   int32_t  d;             /* head dimension: 16, 32, 64 or 128 */
   int32_t  causal;        /* 0 or 1 */

@@ -17,7 +17,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["sbp_api.hip", "sbp_sampler.hip", "sbp_gather.hip", "sbp_linear.hip", "sbp_linear_f32.hip", "sbp_dwconv.hip", "sbp_pointwise.hip", "sbp_attention.hip", "sbp_static.hip",
            "sbp_lm_api.hip", "sbp_lm_attention.hip", "sbp_lm_norm.hip", "sbp_lm_embedding.hip",
-           *[f"sbp_lm_attention_fwd_{d}.hip" for d in (16, 32, 64, 128)]]
+           *[f"sbp_lm_attention_{way}_{d}.hip" for way in ("fwd", "bwd") for d in (16, 32, 64, 128)]]
 LIB = os.path.join(HERE, "libsbp.so")
 NATIVE = os.path.join(HERE, "_native.so")        # the binding of the calls of every step (host code, against torch's headers)
 

@@ -24,6 +24,7 @@ static int32_t validate_masked(const sbp_attention_desc* a, int64_t rows, int32_
   if (a->d != 16 && a->d != 32 && a->d != 64 && a->d != 128) return fail(SBP_ERR_SHAPE, "head dimension must be 16, 32, 64 or 128, got %d", a->d);
   if ((int64_t)a->B * a->n > INT32_MAX) return fail(SBP_ERR_SHAPE, "B*n=%lld exceeds int32 row ids", (long long)a->B * a->n);
   if ((a->h + 2LL * a->h_kv) * a->d > (1 << 24)) return fail(SBP_ERR_SHAPE, "(h + 2 h_kv) * d is too large");
+  if (a->n > (1 << 24)) return fail(SBP_ERR_SHAPE, "n=%d: positions beyond 2^24 are not exact in fp32", a->n);
   if (rows < 0 || rows > a->n) return fail(SBP_ERR_SHAPE, "need 0 <= n_k <= n, got n_k=%lld n=%d", (long long)rows, a->n);
   // (a grid of 256 or 512 threads per 32 tokens and head, in two roles, stays below 2^32 threads)
   if ((int64_t)a->B * a->h * ceil_div(a->n, 32) >= (1 << 22)) return fail(SBP_ERR_SHAPE, "B * h * n is too large for one call");

@@ -1,5 +1,7 @@
 // Masked attention (sbp_lm.h): forward over all tokens of a sample and backward on the kept ones.
-#include "sbp_lm_attention_rows.h"
+#include <algorithm>
+
+#include "sbp_lm_attention_tiles.h"
 
 namespace sbp {
 
@@ -37,7 +39,88 @@ __global__ void __launch_bounds__(256) masked_backward_rows_kernel(MaskedAttenti
   }
 }
 
-MaskedAttentionPlan plan_masked_attention_backward(const sbp_attention_desc&, int32_t, int32_t) { return MaskedAttentionPlan{0}; }
+template <typename T>
+__global__ void __launch_bounds__(256) masked_prepare_kernel(MaskedAttention a, LmTables w) {
+  const int tiles = w.npad / kLmTile, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long long unit = (long long)blockIdx.x * 4 + wave;  // a wavefront per tile and head; head h: positions and documents
+  if (unit >= (long long)a.B * (a.h + 1) * tiles) return;
+  const int tile = (int)(unit % tiles), bh = (int)(unit / tiles), b = bh / (a.h + 1), head = bh % (a.h + 1), t = tile * kLmTile + lane;
+  const bool on = t < a.rows;
+  if (head == a.h) {
+    const int p = on ? lm_pos(a, b, t) : 0, d = on ? lm_doc(a, b, p) : -1;
+    w.pos[(long long)b * w.npad + t] = on ? (float)p : NAN;
+    w.doc[(long long)b * w.npad + t] = d;
+    LmDocs r;
+    if (on) r.add(d);
+    int p0 = on ? p : INT32_MAX, p1 = on ? p : INT32_MIN;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      r.join(m);
+      p0 = min(p0, __shfl_xor(p0, m));
+      p1 = max(p1, __shfl_xor(p1, m));
+    }
+    r.close();
+    if (lane == 0) w.range[(long long)b * tiles + tile] = make_int4(p0, p1, r.lo, r.hi);
+    return;
+  }
+  // delta of a row: d / 8 (bf16) or d / 4 (fp32) lanes of 16 bytes each
+  constexpr int N = 16 / sizeof(T);
+  const int per = a.d / N, rows = 64 / per;
+  const long long ld = (long long)a.h * a.d, row0 = (long long)b * a.rows, at = ((long long)b * a.h + head) * w.npad + tile * kLmTile;
+  for (int r0 = 0; r0 < kLmTile; r0 += rows) {
+    const int row = r0 + lane / per, tok = tile * kLmTile + row, c = lane % per * N;
+    float s = 0.f;
+    if (tok < a.rows) s = lm_dot((const T*)a.dA + (row0 + tok) * ld + head * a.d + c, (const T*)a.A + (row0 + tok) * ld + head * a.d + c, N);
+    for (int m = 1; m < per; m <<= 1) s += __shfl_xor(s, m);
+    if (lane % per == 0) w.nd[at + row] = -s;
+  }
+  const float l = on ? a.lse[(row0 + t) * a.h + head] : -INFINITY;
+  w.l2[at + lane] = l == -INFINITY ? 1e30f : l * kLog2e;    // (a weight of exp2(score - 1e30) = 0)
+}
+
+// Adds the parts of dK and dV of shared heads in order and rounds once: four channels per thread.
+__global__ void __launch_bounds__(256) masked_join_kernel(MaskedAttention a, LmTables w) {
+  const long long pieces = (long long)a.B * a.rows * a.hk * 2 * a.d / 4, i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= pieces) return;
+  float4 s = reinterpret_cast<const float4*>(w.part)[i];
+  for (int p = 1; p < w.parts; ++p) {
+    const float4 v = reinterpret_cast<const float4*>(w.part)[p * pieces + i];
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  const int c = (int)(i * 4 % (2 * a.d)), kv = (int)(i * 4 / (2 * a.d) % a.hk);
+  const long long row = i * 4 / (2 * a.d) / a.hk, ld = (long long)(a.h + 2 * a.hk) * a.d;
+  const int col = c < a.d ? (a.h + kv) * a.d + c : (a.h + a.hk + kv) * a.d + c - a.d;
+  *reinterpret_cast<uint2*>((uint16_t*)a.out + row * ld + col) = make_uint2(bf16_pack(s.x, s.y), bf16_pack(s.z, s.w));
+}
+
+// Parts of a key / value head: its query heads follow one another in one workgroup per 128 keys unless that leaves fewer than two
+// workgroups per CU (256 CUs); then they are dealt to the smallest number of parts that does, each one more set of fp32 dK and dV.
+static int masked_parts(int64_t heads, int share, int nchunks) {
+  int p = 1;
+  while (p < share && heads * p * nchunks < 512) {
+    ++p;
+    while (share % p) ++p;
+  }
+  return p;
+}
+
+MaskedAttentionPlan plan_masked_attention_backward(const sbp_attention_desc& d, int32_t n_k, int32_t dtype) {
+  MaskedAttentionPlan p = {};
+  if (n_k == 0 || dtype != SBP_BF16) return p;
+  p.npad = (int)(ceil_div(n_k, kLmTile) * kLmTile);
+  p.nchunks = (int)ceil_div(n_k, kLmChunk);
+  p.parts = masked_parts((int64_t)d.B * d.h_kv, d.h / d.h_kv, p.nchunks);
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
+  p.off_l2 = take((size_t)d.B * d.h * p.npad * 4);
+  p.off_nd = take((size_t)d.B * d.h * p.npad * 4);
+  p.off_pos = take((size_t)d.B * p.npad * 4);
+  p.off_doc = take((size_t)d.B * p.npad * 4);
+  p.off_range = take((size_t)d.B * (p.npad / kLmTile) * sizeof(int4));
+  p.off_part = take(p.parts > 1 ? (size_t)p.parts * d.B * n_k * d.h_kv * 2 * d.d * 4 : 0);
+  p.bytes = at;
+  return p;
+}
 
 int32_t launch_forward_attention_masked(const MaskedAttention& a, int32_t dtype, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.B * a.h * ceil_div(a.rows, 32)));
@@ -50,10 +133,25 @@ int32_t launch_forward_attention_masked(const MaskedAttention& a, int32_t dtype,
   return check_launch("forward_attention_masked");
 }
 
-int32_t launch_backward_attention_masked(const MaskedAttention& a, const MaskedAttentionPlan&, int32_t dtype, void*, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.B * (a.h + a.hk) * ceil_div(a.rows, 32)));
-  if (dtype == SBP_BF16) SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_backward_rows_kernel<uint16_t>), grid, dim3(256), 0, s, a);
-  else SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_backward_rows_kernel<float>), grid, dim3(256), 0, s, a);
+int32_t launch_backward_attention_masked(const MaskedAttention& a, const MaskedAttentionPlan& p, int32_t dtype, void* ws_, hipStream_t s) {
+  if (dtype == SBP_BF16) {
+    char* ws = (char*)ws_;
+    const LmTables w{(float*)(ws + p.off_l2), (float*)(ws + p.off_nd), (float*)(ws + p.off_pos), (int32_t*)(ws + p.off_doc), (int4*)(ws + p.off_range),
+                     p.parts > 1 ? (float*)(ws + p.off_part) : nullptr, p.npad, p.parts, p.nchunks};
+    const int64_t units = (int64_t)a.B * (a.h + 1) * (p.npad / kLmTile);
+    SBP_LAUNCH(SBP_PROF_OTHER, s, (masked_prepare_kernel<uint16_t>), dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, s, a, w);
+    if (a.d == 16) launch_masked_backward_bf16<16>(a, w, s);
+    else if (a.d == 32) launch_masked_backward_bf16<32>(a, w, s);
+    else if (a.d == 64) launch_masked_backward_bf16<64>(a, w, s);
+    else launch_masked_backward_bf16<128>(a, w, s);
+    if (p.parts > 1) {
+      const int64_t pieces = (int64_t)a.B * a.rows * a.hk * 2 * a.d / 4;
+      SBP_LAUNCH(SBP_PROF_REDUCE, s, masked_join_kernel, dim3((unsigned)ceil_div(pieces, 256)), dim3(256), 0, s, a, w);
+    }
+  } else {
+    const dim3 grid((unsigned)((int64_t)a.B * (a.h + a.hk) * ceil_div(a.rows, 32)));
+    SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_backward_rows_kernel<float>), grid, dim3(256), 0, s, a);
+  }
   return check_launch("backward_attention_masked");
 }
 

@@ -1,0 +1,401 @@
+// Backward of the masked attention on the kept tokens, on the bf16 matrix cores.
+//
+// A small kernel first makes what the others read per token: lse log2(e) and -delta = -dA.A per head (padded to whole tiles of 64 with
+// weights of 0), positions and documents per sample, and their ranges per tile.
+// A workgroup of 4 wavefronts owns 128 tokens of one sample, every wavefront 32, in one of two roles: as keys of a key / value head (dK,
+// dV; the rows of q and dA of its query heads stream through LDS) or as queries of a query head (dQ; k and v stream).  Layouts as in
+// sbp_attention.hip: own tokens are the columns (lanes) of every product, streamed ones the rows (registers), so that P and dM are,
+// packed to bf16 (one rounding of 2^-8, the matrix cores multiply bf16), the B operands of the products that follow.  Recomputing S and
+// dP in the second role costs 2 of 7 products and saves every sum across workgroups: no atomics, deterministic.
+// Query heads that share a key / value head follow one another in the stream of its key role; where that leaves too few workgroups, they
+// are dealt to several whose dK and dV, in fp32, a last small kernel adds in order.
+// The loop is a pipeline over blocks of 32 streamed tokens: while the scores of block b turn into weights on the vector units, the matrix
+// cores multiply the weights of block b - 1 and the scores of block b + 1, instruction by instruction in turn.  A tile of two blocks
+// stays three tiles long in a ring of three; one barrier per tile.
+// Tiles of which the workgroup sees nothing are left out of the list (ranges of positions and documents per tile; any order of the kept
+// tokens is right, ascending order makes it short).  Tiles that are visible altogether come first, in a loop without mask arithmetic.
+// Where a result is not finite, its row is computed again one row at a time (see sbp_lm_attention_fwd.h).
+#ifndef SBP_LM_ATTENTION_BWD_H_
+#define SBP_LM_ATTENTION_BWD_H_
+
+#include "sbp_lm_attention_tiles.h"
+
+namespace sbp {
+
+static constexpr int kLmBwdList = 256;                     // tiles per list (16384 tokens); longer samples take several
+
+enum { LM_BWD_CAP = 1, LM_BWD_BIAS = 2 };
+
+template <int D>
+struct LmBwd {
+  using L = AttnSwizzled<D>;
+  using S = LmStream<D, 4>;
+  static constexpr int TABLE = 2 * S::IMG, STAGE = TABLE + 4 * 4 * kLmTile;   // two images, then l2, nd, pos, doc of the tile's tokens
+  static constexpr int OUT = 4 * 2 * 32 * (2 * D + 16);
+  static constexpr size_t LDS = 3 * STAGE > OUT ? 3 * STAGE : OUT;
+};
+
+template <int D, bool KEY, int MODE>
+__device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, int* count_s, const MaskedAttention& a, const LmTables& w, int b, int group,
+                                                     int chunk) {
+  using F = LmBwd<D>;
+  using L = AttnSwizzled<D>;
+  constexpr int KS = L::KS, DB = L::DB;
+  constexpr bool CAP = MODE & LM_BWD_CAP, BIAS = MODE & LM_BWD_BIAS;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), u = lane >> 5;
+  const int rows = a.rows, tiles = w.npad / kLmTile, ld = (a.h + 2 * a.hk) * D, lda = a.h * D, share = a.h / a.hk;
+  // heads of the stream (KEY) or the head of the queries
+  const int nh = KEY ? share / w.parts : 1;
+  const int kv = KEY ? group / w.parts : group / share;
+  const int h0 = KEY ? kv * share + group % w.parts * nh : group;
+  const long long row0 = (long long)b * rows;
+  const uint16_t* qkv = (const uint16_t*)a.qkv + row0 * ld;
+  const uint16_t* dA = (const uint16_t*)a.dA + row0 * lda;
+  const int first = chunk * kLmChunk + wave * 32, mine = first + (lane & 31), own = min(mine, rows - 1);
+  const bool busy = first < rows, docs = a.doc != nullptr;
+  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const L lay(lane);
+  const uint32_t lds0 = lm_lds(smem);
+
+  bf16x8_t f1[KS], f2[KS];                                  // k, v (KEY) or q, dA of the own token
+  {
+    const uint16_t* p1 = qkv + (long long)own * ld + (KEY ? a.h + kv : h0) * D + 8 * u;
+    const uint16_t* p2 = KEY ? p1 + a.hk * D : dA + (long long)own * lda + h0 * D + 8 * u;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      f1[ks] = *reinterpret_cast<const bf16x8_t*>(p1 + 16 * ks);
+      f2[ks] = *reinterpret_cast<const bf16x8_t*>(p2 + 16 * ks);
+    }
+  }
+  const float own_pos = w.pos[(long long)b * w.npad + own];
+  const int own_doc = w.doc[(long long)b * w.npad + own];
+  // streamed positions >= bound (KEY) or <= bound are visible
+  float bound = KEY ? -3e38f : 3e38f;
+  if (a.causal) bound = KEY ? (own_pos < (float)prefix ? -3e38f : own_pos) : fmaxf(own_pos, (float)prefix - 1.f);
+  if (docs && own_doc < 0) bound = KEY ? 3e38f : -3e38f;
+  float own_l2 = 0.f;
+  f32x16_t nd;                                              // QUERY: -delta in every register
+  if constexpr (!KEY) {
+    own_l2 = w.l2[((long long)b * a.h + h0) * w.npad + own];
+    const float v = w.nd[((long long)b * a.h + h0) * w.npad + own];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      nd[e] = v;
+      asm("" : "+v"(nd[e]));                                // (16 registers for good: as one value it would be copied 16 times per block)
+    }
+  }
+  const float c2 = a.scale * kLog2e, cap2 = a.cap * kLog2e, ct = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f;
+
+  constexpr int NACC = KEY ? 2 : 1;
+  f32x16_t acc[NACC][DB];                                   // dK, dV or dQ: rows head dim, columns own tokens
+#pragma unroll
+  for (int q = 0; q < NACC; ++q)
+#pragma unroll
+    for (int x = 0; x < DB; ++x)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[q][x][e] = 0.f;
+  f32x16_t sc, dp;                                          // scores and dP of the block whose weights come next
+  bf16x8_t pw[2], ds[2];                                    // P and dM of the block before
+
+  // One turn of the pipeline: products of the block before (pt: its tile, pj: its first row), weights of the block whose scores are there
+  // (wt, wj), scores of the next one (st, sj).  Operands are read kAhead products before they are multiplied.
+  auto turn = [&](auto masked_, const char* pt, int pj, const char* wt, int wj, float slope2, const char* st, int sj) {
+    constexpr bool MASKED = decltype(masked_)::value;
+    constexpr int NP = 2 * DB * NACC, N = NP + 2 * KS, AHEAD = 6 < N ? 6 : N;
+    auto operand = [&](int i) {
+      if (i < NP) {
+        const int x = i % DB, q = i / DB % NACC, ks = i / DB / NACC;
+        return lay.tr(pt + (q ? F::S::IMG : 0), pj + 16 * ks, x);
+      }
+      const int j = i - NP;
+      return lay.row(st + (j & 1 ? F::S::IMG : 0), sj, j >> 1);
+    };
+    const float* tab = reinterpret_cast<const float*>(wt + F::TABLE) + wj + 4 * u;
+    f32x16_t sn, dn;
+    if constexpr (KEY) {
+      const float* nt = reinterpret_cast<const float*>(st + F::TABLE) + kLmTile + sj + 4 * u;
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(nt + 8 * q4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dn[4 * q4 + e] = v[e];
+      }
+    } else {
+      dn = nd;
+    }
+    const f32x16_t zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    // the tokens' table, four rows at a time, read one group ahead (positions and documents where they are used)
+    f32x4_t tl[2], tp[2];
+    int4 td[2];
+    auto table = [&](int q4) {
+      if constexpr (KEY) tl[q4 & 1] = *reinterpret_cast<const f32x4_t*>(tab + 8 * q4);
+      if constexpr (BIAS || MASKED) tp[q4 & 1] = *reinterpret_cast<const f32x4_t*>(tab + 2 * kLmTile + 8 * q4);
+      if constexpr (MASKED) td[q4 & 1] = *reinterpret_cast<const int4*>(tab + 3 * kLmTile + 8 * q4);
+    };
+    table(0);
+    bf16x8_t f[AHEAD], pn[2], mn[2];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) f[i] = operand(i);
+    // the weights, register e: 16 steps dealt out over the products
+    auto weight = [&](int e) {
+      const int q4 = e >> 2, i = e & 3;
+      if (i == 0 && q4 < 3) table(q4 + 1);
+      const float l2 = KEY ? tl[q4 & 1][i] : own_l2;
+      float x, slope = 1.f;
+      if constexpr (CAP) {
+        const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(sc[e] * ct) + 1.f);
+        x = fmaf(-2.f * cap2, r, cap2) - l2;                 // cap tanh(z / cap)
+        slope = fmaf(-r, r, r);                              // (1 - tanh^2) / 4
+      } else {
+        x = fmaf(sc[e], c2, -l2);
+      }
+      if constexpr (BIAS) x = fmaf(-slope2, fabsf(tp[q4 & 1][i] - own_pos), x);
+      float p = __builtin_amdgcn_exp2f(x), m = p * dp[e];
+      if constexpr (CAP) m *= slope;
+      if constexpr (MASKED) {
+        const int dj = i == 0 ? td[q4 & 1].x : i == 1 ? td[q4 & 1].y : i == 2 ? td[q4 & 1].z : td[q4 & 1].w;
+        const bool see = (KEY ? tp[q4 & 1][i] >= bound : tp[q4 & 1][i] <= bound) && dj == own_doc;
+        p = see ? p : 0.f;
+        m = see ? m : 0.f;
+      }
+      sc[e] = p;
+      dp[e] = m;
+      if (e == 7 || e == 15) {
+        if constexpr (KEY) pn[e >> 3] = pack8(sc, e >> 3);
+        mn[e >> 3] = pack8(dp, e >> 3);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < NP) {
+        const int x = i % DB, q = i / DB % NACC, ks = i / DB / NACC;
+        acc[q][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], q ? pw[ks] : ds[ks], acc[q][x], 0, 0, 0);
+      } else {
+        const int j = i - NP;
+        if (j & 1) dn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], f2[j >> 1], dn, 0, 0, 0);
+        else sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], f1[j >> 1], j ? sn : zero, 0, 0, 0);
+      }
+      if (i + AHEAD < N) f[i % AHEAD] = operand(i + AHEAD);
+#pragma unroll
+      for (int e = 16 * i / N; e < 16 * (i + 1) / N; ++e) weight(e);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      if constexpr (KEY) pw[ks] = pn[ks];
+      ds[ks] = mn[ks];
+    }
+    sc = sn;
+    dp = dn;
+  };
+
+  const int4* ranges = w.range + (long long)b * tiles;
+  LmRange mr[2];                                            // the two halves of the chunk
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const int4 r = ranges[min(2 * chunk + y, tiles - 1)];
+    mr[y] = LmRange{r.x, r.y, r.z, r.w};
+  }
+  for (int base = 0; base < tiles; base += kLmBwdList) {
+    const int here = min(kLmBwdList, tiles - base);
+    // the list: first the tiles that are visible altogether, from its front, then the others, from its back
+    if (wave == 0) {
+      int count = 0, back = 0;
+      for (int i0 = 0; i0 < here; i0 += 64) {
+        const int i = i0 + lane;
+        const int4 e = ranges[base + min(i, here - 1)];
+        const LmRange r{e.x, e.y, e.z, e.w};
+        int cls[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) cls[y] = KEY ? lm_class(r, mr[y], a.causal, prefix, docs) : lm_class(mr[y], r, a.causal, prefix, docs);
+        const bool on = i < here && (cls[0] | cls[1]), full = on && cls[0] == 2 && cls[1] == 2 && (base + i + 1) * kLmTile <= rows;
+        const unsigned long long m = __ballot(full), v = __ballot(on && !full), below = (1ull << lane) - 1;
+        if (full) list_s[count + __popcll(m & below)] = base + i;
+        else if (on) list_s[kLmBwdList - 1 - back - __popcll(v & below)] = base + i;
+        count += __popcll(m);
+        back += __popcll(v);
+      }
+      if (lane == 0) { count_s[0] = count; count_s[1] = back; }
+    }
+    __syncthreads();
+    const int nf = __builtin_amdgcn_readfirstlane(count_s[0]), nm = __builtin_amdgcn_readfirstlane(count_s[1]), total = (nf + nm) * nh;
+    if (total > 0) {
+      // the stream: the visible tiles for every head, then the masked ones for every head
+      struct Place { int head, i, masked; };
+      auto entry = [&](const Place& p) { return __builtin_amdgcn_readfirstlane(list_s[p.masked ? kLmBwdList - 1 - p.i : p.i]); };
+      auto advance = [&](Place& p) {
+        if (++p.i < (p.masked ? nm : nf)) return;
+        p.i = 0;
+        if (++p.head < h0 + nh) return;
+        p.head = h0;
+        p.masked = 1;
+      };
+      auto issue = [&](int s, const Place& p) {
+        const int t0 = entry(p) * kLmTile, head = p.head;
+        const uint32_t buf = lds0 + s % 3 * F::STAGE;
+        F::S::issue_one(qkv + (KEY ? head : a.h + kv) * D, ld, t0, rows, buf, lane, wave);
+        if constexpr (KEY) F::S::issue_one(dA + head * D, lda, t0, rows, buf + F::S::IMG, lane, wave);
+        else F::S::issue_one(qkv + (a.h + a.hk + kv) * D, ld, t0, rows, buf + F::S::IMG, lane, wave);
+        if (wave == (s & 3)) {
+          const long long th = ((long long)b * a.h + head) * w.npad + t0, tb = (long long)b * w.npad + t0;
+          const char* src = lane < 16 ? (const char*)(w.l2 + th) : lane < 32 ? (const char*)(w.nd + th) : lane < 48 ? (const char*)(w.pos + tb) : (const char*)(w.doc + tb);
+          lm_copy16(src + 16 * (lane & 15), buf + F::TABLE);
+        }
+      };
+      auto image = [&](int s) { return smem + s % 3 * F::STAGE; };
+      Place coming{h0, 0, nf == 0}, at = coming;            // of the next tile to copy, of the one whose weights come next
+      issue(0, coming);
+      advance(coming);
+      if (total > 1) { issue(1, coming); advance(coming); }
+      wait_async_copies<0>();
+      lm_copies_done();
+      lds_barrier();
+      if (busy) {
+        // the pipeline's first scores; the products of the turn before them are of weights 0
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pw[ks][e] = ds[ks][e] = (__bf16)0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+        if constexpr (KEY) {
+          const float* nt = reinterpret_cast<const float*>(image(0) + F::TABLE) + kLmTile + 4 * u;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) dp[e] = nt[8 * (e >> 2) + (e & 3)];
+        } else {
+          dp = nd;
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.row(image(0), 0, ks), f1[ks], sc, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.row(image(0) + F::S::IMG, 0, ks), f2[ks], dp, 0, 0, 0);
+        }
+      }
+      auto block = [&](auto masked_, int k) {                // block k: half k & 1 of tile s
+        const int s = k >> 1, j = (k & 1) * 32;
+        if (j) {
+          lm_copies_done();                                 // tile s + 1 ...
+          lds_barrier();                                    // ... everywhere; the place of tile s - 1 is free
+          if (s + 2 < total) { issue(s + 2, coming); advance(coming); }
+        }
+        if (busy) {
+          const float slope2 = BIAS ? a.slopes[at.head] * kLog2e : 0.f;
+          const char* now = image(s);
+          // (before the first block its own rows stand for the block before, after the last one for the block after)
+          turn(masked_, j || !s ? now : image(s + 2), j ? 0 : s ? 32 : 0, now, j, slope2, j && s + 1 < total ? image(s + 1) : now, 32 - j);
+        }
+        if (j) advance(at);
+      };
+#pragma unroll 1
+      for (int k = 0; k < 2 * nf * nh; ++k) block(std::false_type{}, k);
+#pragma unroll 1
+      for (int k = 2 * nf * nh; k < 2 * total; ++k) block(std::true_type{}, k);
+      if (busy) {
+        const char* last = image(total - 1);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int x = 0; x < DB; ++x) {
+            acc[0][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.tr(last, 32 + 16 * ks, x), ds[ks], acc[0][x], 0, 0, 0);
+            if constexpr (KEY) acc[1][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.tr(last + F::S::IMG, 32 + 16 * ks, x), pw[ks], acc[1][x], 0, 0, 0);
+          }
+      }
+    }
+    __syncthreads();                                        // the tiles and the list have been consumed
+  }
+  if (!busy) return;
+  bool fine = true;
+#pragma unroll
+  for (int q = 0; q < NACC; ++q)
+#pragma unroll
+    for (int x = 0; x < DB; ++x)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (D >= 32 || e < 8) fine = fine && lm_finite(acc[q][x][e]);
+  unsigned long long again = __ballot(!fine);
+  again = (again | again >> 32) & 0xffffffffull;
+  const float dscale = CAP ? 4.f * a.scale : a.scale;
+  uint16_t* out = (uint16_t*)a.out + row0 * ld;
+  char* img = smem + wave * (2 * 32 * (2 * D + 16));
+  if constexpr (!KEY) {
+    attn_store_rows<D>(img, acc[0], dscale, out + h0 * D, ld, first, rows, lane);
+    for (; again; again &= again - 1) {
+      const int q = first + __ffsll((long long)again) - 1;
+      if (q < rows) lm_backward_query<uint16_t>(a, b, h0, q, lane);
+    }
+  } else {
+    float* part = w.part ? w.part + (((long long)(group % w.parts) * a.B + b) * rows * a.hk + kv) * (2 * D) : nullptr;
+    if (!part) {
+      attn_store_rows<D>(img, acc[0], dscale, out + (a.h + kv) * D, ld, first, rows, lane);
+      attn_store_rows<D>(img + 32 * (2 * D + 16), acc[1], 1.f, out + (a.h + a.hk + kv) * D, ld, first, rows, lane);
+    } else if (mine < rows) {
+      float* p = part + (long long)mine * (a.hk * 2 * D) + 4 * u;
+#pragma unroll
+      for (int x = 0; x < DB; ++x)
+#pragma unroll
+        for (int q4 = 0; q4 < (D < 32 ? D / 8 : 4); ++q4) {
+          *reinterpret_cast<float4*>(p + 32 * x + 8 * q4) = make_float4(acc[0][x][4 * q4] * dscale, acc[0][x][4 * q4 + 1] * dscale, acc[0][x][4 * q4 + 2] * dscale, acc[0][x][4 * q4 + 3] * dscale);
+          *reinterpret_cast<float4*>(p + D + 32 * x + 8 * q4) = make_float4(acc[1][x][4 * q4], acc[1][x][4 * q4 + 1], acc[1][x][4 * q4 + 2], acc[1][x][4 * q4 + 3]);
+        }
+    }
+    for (; again; again &= again - 1) {
+      const int j = first + __ffsll((long long)again) - 1;
+      if (j >= rows) continue;
+      float dk[2], dv[2];
+      lm_backward_key<uint16_t>(a, b, kv, h0, h0 + nh, j, lane, dk, dv);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int c = lane + 64 * e;
+        if (c >= D) continue;
+        if (part) {
+          part[(long long)j * (a.hk * 2 * D) + c] = dk[e];
+          part[(long long)j * (a.hk * 2 * D) + D + c] = dv[e];
+        } else {
+          lm_store(out + (long long)j * ld + (a.h + kv) * D + c, dk[e]);
+          lm_store(out + (long long)j * ld + (a.h + a.hk + kv) * D + c, dv[e]);
+        }
+      }
+    }
+  }
+}
+
+template <int D, int MODE>
+__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) masked_backward_kernel(MaskedAttention a, LmTables w) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ int list_s[kLmBwdList], count_s[2];
+  // units of one rank: the key groups and the query heads of all samples; the heads of one XCD stay on it where both divide by 8
+  const int nk = a.B * a.hk * w.parts, nq = a.B * a.h, i = blockIdx.x;
+  int rank, k;
+  if (nk % 8 == 0 && nq % 8 == 0) {
+    const int pk = nk / 8, pq = nq / 8, j = i >> 3, x = i & 7;
+    rank = j / (pk + pq);
+    k = j % (pk + pq);
+    k = k < pk ? x * pk + k : nk + x * pq + k - pk;
+  } else {
+    rank = i / (nk + nq);
+    k = i % (nk + nq);
+  }
+  // causal: the first keys are seen by the most queries, the last queries see the most keys
+  if (k < nk) masked_backward_body<D, true, MODE>(smem, list_s, count_s, a, w, k / (a.hk * w.parts), k % (a.hk * w.parts), rank);
+  else masked_backward_body<D, false, MODE>(smem, list_s, count_s, a, w, (k - nk) / a.h, (k - nk) % a.h, a.causal ? w.nchunks - 1 - rank : rank);
+}
+
+template <int D, int MODE>
+static void launch_masked_backward(const MaskedAttention& a, const LmTables& w, hipStream_t s) {
+  constexpr size_t lds = LmBwd<D>::LDS;
+  allow_dynamic_lds(reinterpret_cast<const void*>(masked_backward_kernel<D, MODE>), lds);
+  SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_backward_kernel<D, MODE>), dim3((unsigned)((int64_t)w.nchunks * a.B * (a.hk * w.parts + a.h))), dim3(256), lds, s,
+             a, w);
+}
+template <int D>
+void launch_masked_backward_bf16(const MaskedAttention& a, const LmTables& w, hipStream_t s) {
+  const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
+  if (cap && bias) launch_masked_backward<D, LM_BWD_CAP | LM_BWD_BIAS>(a, w, s);
+  else if (cap) launch_masked_backward<D, LM_BWD_CAP>(a, w, s);
+  else if (bias) launch_masked_backward<D, LM_BWD_BIAS>(a, w, s);
+  else launch_masked_backward<D, 0>(a, w, s);
+}
+
+}  // namespace sbp
+#endif

@@ -10,6 +10,18 @@ namespace sbp {
 
 static constexpr int kLmTile = 64;                         // streamed tokens per tile
 
+static constexpr int kLmChunk = 128;                       // own tokens per workgroup of the backward
+
+// What the first kernel of the backward writes (workspace): npad = rows rounded up to whole tiles.
+struct LmTables {
+  float *l2, *nd;                // [B*h][npad]
+  float* pos;                    // [B][npad], NaN past the last token: no comparison with it is true
+  int32_t* doc;                  // [B][npad]
+  int4* range;                   // [B][npad / 64]: positions, documents (0, 0 without documents) of the tile's tokens
+  float* part;                   // [parts][B*rows][hk][2][D]: dK, dV of the parts of a key / value head
+  int npad, parts, nchunks;
+};
+
 // Positions and documents of some tokens, as ranges: positions p0 .. p1; documents d0 .. d1 of the tokens that belong to one (none:
 // d0 > d1), made wider where others belong to none, so that d0 = d1 means that all of them belong to that one.
 struct LmRange {

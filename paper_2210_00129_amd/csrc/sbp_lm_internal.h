@@ -22,10 +22,14 @@ struct MaskedAttention {
   float scale, cap;
 };
 struct MaskedAttentionPlan {     // workspace of the backward
-  size_t bytes;
+  int    npad, nchunks;          // kept tokens per sample in whole tiles; chunks of own tokens per workgroup
+  int    parts;                  // workgroups that share a key / value head's query heads
+  size_t off_l2, off_nd, off_pos, off_doc, off_range, off_part, bytes;
 };
+struct LmTables;
 MaskedAttentionPlan plan_masked_attention_backward(const sbp_attention_desc& a, int32_t n_k, int32_t dtype);
 template <int D> void launch_masked_forward_bf16(const MaskedAttention& a, hipStream_t s);
+template <int D> void launch_masked_backward_bf16(const MaskedAttention& a, const LmTables& w, hipStream_t s);
 int32_t launch_forward_attention_masked(const MaskedAttention& a, int32_t dtype, hipStream_t s);
 int32_t launch_backward_attention_masked(const MaskedAttention& a, const MaskedAttentionPlan& p, int32_t dtype, void* ws, hipStream_t s);
 
