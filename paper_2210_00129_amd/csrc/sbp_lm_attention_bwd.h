@@ -56,6 +56,9 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
   const int prefix = a.prefix ? a.prefix[b] : 0;
   const L lay(lane);
   const uint32_t lds0 = lm_lds(smem);
+  const typename F::S st1(ld, lane, wave), st2(lda, lane, wave);
+  const char* tables[4] = {(const char*)w.l2, (const char*)w.nd, (const char*)w.pos, (const char*)w.doc};
+  const uint32_t table_off = (uint32_t)(tables[lane >> 4] - tables[0]) + 16 * (lane & 15);
 
   bf16x8_t f1[KS], f2[KS];                                  // k, v (KEY) or q, dA of the own token
   {
@@ -97,20 +100,34 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
   f32x16_t sc, dp;                                          // scores and dP of the block whose weights come next
   bf16x8_t pw[2], ds[2];                                    // P and dM of the block before
 
-  // One turn of the pipeline: products of the block before (pt: its tile, pj: its first row), weights of the block whose scores are there
-  // (wt, wj), scores of the next one (st, sj).  Operands are read kAhead products before they are multiplied.
-  auto turn = [&](auto masked_, const char* pt, int pj, const char* wt, int wj, float slope2, const char* st, int sj) {
+  // One turn of the pipeline: products of the block before (in tile pt, first row pj), weights of the block whose scores are there (wt, wj:
+  // half 0 or 1 of its tile), scores of the next one (st, sj).  Operands are read AHEAD
+  // products before they are multiplied, the first ones of a turn (and the first rows of its table) at the end of the turn before: a
+  // product takes 32 cycles, a read of LDS under way some 150.
+  constexpr int NP = 2 * DB * NACC, N = NP + 2 * KS, AHEAD = D == 128 ? 8 : D == 64 ? 4 : 2;
+  static_assert(AHEAD <= NP && N % AHEAD == 0, "the operands read ahead are products' and keep their places from turn to turn");
+  bf16x8_t f[AHEAD];
+  f32x4_t tl[2], tp[2];                                     // the tokens' table, four rows at a time: lse, positions, documents
+  int4 td[2];
+  auto product_operand = [&](int i, const char* tile, int row) {
+    const int x = i % DB, q = i / DB % NACC, ks = i / DB / NACC;
+    return lay.tr(tile + (q ? F::S::IMG : 0), row + 16 * ks, x);
+  };
+  auto table = [&](bool masked, const char* tile, int row, int q4) {
+    const float* tab = reinterpret_cast<const float*>(tile + F::TABLE) + row + 4 * u + 8 * q4;
+    if constexpr (KEY) tl[q4 & 1] = *reinterpret_cast<const f32x4_t*>(tab);
+    if (BIAS || masked) tp[q4 & 1] = *reinterpret_cast<const f32x4_t*>(tab + 2 * kLmTile);
+    if (masked) td[q4 & 1] = *reinterpret_cast<const int4*>(tab + 3 * kLmTile);
+  };
+  auto turn = [&](auto masked_, auto half_, const char* pt, const char* wt, float slope2, const char* st) {
     constexpr bool MASKED = decltype(masked_)::value;
-    constexpr int NP = 2 * DB * NACC, N = NP + 2 * KS, AHEAD = 6 < N ? 6 : N;
-    auto operand = [&](int i) {
-      if (i < NP) {
-        const int x = i % DB, q = i / DB % NACC, ks = i / DB / NACC;
-        return lay.tr(pt + (q ? F::S::IMG : 0), pj + 16 * ks, x);
-      }
+    constexpr int wj = 32 * decltype(half_)::value, pj = 32 - wj, sj = 32 - wj;
+    auto operand = [&](int i) {                              // (from N on: of the next turn, whose block before is this one's)
+      if (i < NP) return product_operand(i, pt, pj);
+      if (i >= N) return product_operand(i - N, wt, wj);
       const int j = i - NP;
       return lay.row(st + (j & 1 ? F::S::IMG : 0), sj, j >> 1);
     };
-    const float* tab = reinterpret_cast<const float*>(wt + F::TABLE) + wj + 4 * u;
     f32x16_t sn, dn;
     if constexpr (KEY) {
       const float* nt = reinterpret_cast<const float*>(st + F::TABLE) + kLmTile + sj + 4 * u;
@@ -124,22 +141,14 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
       dn = nd;
     }
     const f32x16_t zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    // the tokens' table, four rows at a time, read one group ahead (positions and documents where they are used)
-    f32x4_t tl[2], tp[2];
-    int4 td[2];
-    auto table = [&](int q4) {
-      if constexpr (KEY) tl[q4 & 1] = *reinterpret_cast<const f32x4_t*>(tab + 8 * q4);
-      if constexpr (BIAS || MASKED) tp[q4 & 1] = *reinterpret_cast<const f32x4_t*>(tab + 2 * kLmTile + 8 * q4);
-      if constexpr (MASKED) td[q4 & 1] = *reinterpret_cast<const int4*>(tab + 3 * kLmTile + 8 * q4);
-    };
-    table(0);
-    bf16x8_t f[AHEAD], pn[2], mn[2];
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) f[i] = operand(i);
+    bf16x8_t pn[2], mn[2];
     // the weights, register e: 16 steps dealt out over the products
     auto weight = [&](int e) {
       const int q4 = e >> 2, i = e & 3;
-      if (i == 0 && q4 < 3) table(q4 + 1);
+      if (i == 0) {                                          // the next rows: of this block, or of the next one (in tile st)
+        if (q4 < 3) table(MASKED, wt, wj, q4 + 1);
+        else table(MASKED, st, sj, 0);
+      }
       const float l2 = KEY ? tl[q4 & 1][i] : own_l2;
       float x, slope = 1.f;
       if constexpr (CAP) {
@@ -176,7 +185,7 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
         if (j & 1) dn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], f2[j >> 1], dn, 0, 0, 0);
         else sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], f1[j >> 1], j ? sn : zero, 0, 0, 0);
       }
-      if (i + AHEAD < N) f[i % AHEAD] = operand(i + AHEAD);
+      f[i % AHEAD] = operand(i + AHEAD);
 #pragma unroll
       for (int e = 16 * i / N; e < 16 * (i + 1) / N; ++e) weight(e);
     }
@@ -231,23 +240,22 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
         p.head = h0;
         p.masked = 1;
       };
-      auto issue = [&](int s, const Place& p) {
+      auto issue = [&](int s, const Place& p) {             // into the place at byte s of the ring
         const int t0 = entry(p) * kLmTile, head = p.head;
-        const uint32_t buf = lds0 + s % 3 * F::STAGE;
-        F::S::issue_one(qkv + (KEY ? head : a.h + kv) * D, ld, t0, rows, buf, lane, wave);
-        if constexpr (KEY) F::S::issue_one(dA + head * D, lda, t0, rows, buf + F::S::IMG, lane, wave);
-        else F::S::issue_one(qkv + (a.h + a.hk + kv) * D, ld, t0, rows, buf + F::S::IMG, lane, wave);
-        if (wave == (s & 3)) {
-          const long long th = ((long long)b * a.h + head) * w.npad + t0, tb = (long long)b * w.npad + t0;
-          const char* src = lane < 16 ? (const char*)(w.l2 + th) : lane < 32 ? (const char*)(w.nd + th) : lane < 48 ? (const char*)(w.pos + tb) : (const char*)(w.doc + tb);
-          lm_copy16(src + 16 * (lane & 15), buf + F::TABLE);
+        const uint32_t buf = lds0 + (uint32_t)s;
+        st1.issue(qkv + (KEY ? head : a.h + kv) * D, t0, rows, buf, lane, wave);
+        if constexpr (KEY) st2.issue(dA + head * D, t0, rows, buf + F::S::IMG, lane, wave);
+        else st1.issue(qkv + (a.h + a.hk + kv) * D, t0, rows, buf + F::S::IMG, lane, wave);
+        if (wave == 3) {
+          // (the tables lie within 2^31 bytes of each other)
+          const uint32_t th = 4u * (uint32_t)((b * a.h + head) * w.npad + t0), tb = 4u * (uint32_t)(b * w.npad + t0);
+          lm_copy16(w.l2, table_off + (lane < 32 ? th : tb), buf + F::TABLE);
         }
       };
-      auto image = [&](int s) { return smem + s % 3 * F::STAGE; };
       Place coming{h0, 0, nf == 0}, at = coming;            // of the next tile to copy, of the one whose weights come next
       issue(0, coming);
       advance(coming);
-      if (total > 1) { issue(1, coming); advance(coming); }
+      if (total > 1) { issue(F::STAGE, coming); advance(coming); }
       wait_async_copies<0>();
       lm_copies_done();
       lds_barrier();
@@ -260,7 +268,7 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[e] = 0.f;
         if constexpr (KEY) {
-          const float* nt = reinterpret_cast<const float*>(image(0) + F::TABLE) + kLmTile + 4 * u;
+          const float* nt = reinterpret_cast<const float*>(smem + F::TABLE) + kLmTile + 4 * u;
 #pragma unroll
           for (int e = 0; e < 16; ++e) dp[e] = nt[8 * (e >> 2) + (e & 3)];
         } else {
@@ -268,31 +276,36 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.row(image(0), 0, ks), f1[ks], sc, 0, 0, 0);
-          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.row(image(0) + F::S::IMG, 0, ks), f2[ks], dp, 0, 0, 0);
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.row(smem, 0, ks), f1[ks], sc, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lay.row(smem + F::S::IMG, 0, ks), f2[ks], dp, 0, 0, 0);
         }
       }
-      auto block = [&](auto masked_, int k) {                // block k: half k & 1 of tile s
-        const int s = k >> 1, j = (k & 1) * 32;
-        if (j) {
-          lm_copies_done();                                 // tile s + 1 ...
-          lds_barrier();                                    // ... everywhere; the place of tile s - 1 is free
-          if (s + 2 < total) { issue(s + 2, coming); advance(coming); }
-        }
-        if (busy) {
-          const float slope2 = BIAS ? a.slopes[at.head] * kLog2e : 0.f;
-          const char* now = image(s);
-          // (before the first block its own rows stand for the block before, after the last one for the block after)
-          turn(masked_, j || !s ? now : image(s + 2), j ? 0 : s ? 32 : 0, now, j, slope2, j && s + 1 < total ? image(s + 1) : now, 32 - j);
-        }
-        if (j) advance(at);
+      int before = 0, now = 0, after = F::STAGE, left = total;      // places of the tile before (at first: any), of this one, of the next
+      auto tile = [&](auto masked_) {
+        const float slope2 = BIAS ? a.slopes[at.head] * kLog2e : 0.f;
+        if (busy) turn(masked_, std::integral_constant<int, 0>{}, smem + before, smem + now, slope2, smem + now);
+        lm_copies_done();                                   // the next tile ...
+        lds_barrier();                                      // ... everywhere; the place of the one before is free
+        const int over = 3 * F::STAGE - now - after;
+        if (left > 2) { issue(over, coming); advance(coming); }
+        // (after the last block its tile's own rows stand for the next scores, which nothing uses)
+        if (busy) turn(masked_, std::integral_constant<int, 1>{}, smem + now, smem + now, slope2, smem + (left > 1 ? after : now));
+        before = now; now = after; after = over;
+        --left;
+        advance(at);
       };
-#pragma unroll 1
-      for (int k = 0; k < 2 * nf * nh; ++k) block(std::false_type{}, k);
-#pragma unroll 1
-      for (int k = 2 * nf * nh; k < 2 * total; ++k) block(std::true_type{}, k);
       if (busy) {
-        const char* last = image(total - 1);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) f[i] = product_operand(i, smem, 32);
+        table(true, smem, 0, 0);
+      }
+#pragma unroll 1
+      for (int s = 0; s < nf * nh; ++s) tile(std::false_type{});
+      if (busy && nf) table(true, smem + now, 0, 0);         // (the loop before read less of it)
+#pragma unroll 1
+      for (int s = 0; s < nm * nh; ++s) tile(std::true_type{});
+      if (busy) {
+        const char* last = smem + before;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll

@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
   const int di = docs ? doc[own] : 0;
   const L lay(lane);
   const uint32_t lds0 = lm_lds(smem);
+  const typename F::S st(ld, lane, wave);
   bf16x8_t qf[KS];
   {
     const uint16_t* q = base + (long long)own * ld + head * D + 8 * u;
@@ -243,10 +244,10 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
       const uint32_t buf = lds0 + (s & 1) * F::STAGE;
       if (s < ns) {
         const int t0 = (base_tile + tile) * kLmTile;
-        F::S::issue_one(k0, ld, t0, n, buf, lane, wave);
-        if (docs && wave == s % NW) lm_copy4(doc + min(t0 + lane, n - 1), lds0 + F::DOCS + (s & 3) * (4 * kLmTile));
+        st.issue(k0, t0, n, buf, lane, wave);
+        if (docs && wave == s % NW) lm_copy4(doc + t0, 4u * min(lane, n - 1 - t0), lds0 + F::DOCS + (s & 3) * (4 * kLmTile));
       }
-      if (s > 0 && s <= ns) F::S::issue_one(v0, ld, (base_tile + before) * kLmTile, n, buf + F::S::IMG, lane, wave);
+      if (s > 0 && s <= ns) st.issue(v0, (base_tile + before) * kLmTile, n, buf + F::S::IMG, lane, wave);
     };
         int copied = __builtin_amdgcn_readfirstlane(entry(0).x), coming = __builtin_amdgcn_readfirstlane(entry(1).x);
     issue(0, copied, 0);

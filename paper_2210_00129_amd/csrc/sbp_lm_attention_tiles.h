@@ -68,11 +68,12 @@ __device__ __forceinline__ void lm_unit(unsigned i, int heads, int* rank, int* h
 // and barriers; both keep the compiler from moving LDS reads across them.  An address is read when its copy is issued; m0 is a register
 // that the compiler sets right before each of its own uses.
 __device__ __forceinline__ uint32_t lm_lds(const char* p) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uintptr_t)(SBP_LDS const char*)p); }
-__device__ __forceinline__ void lm_copy16(const void* g, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(to) : "memory");
+// base: wave-uniform; off: bytes, per lane
+__device__ __forceinline__ void lm_copy16(const void* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory");
 }
-__device__ __forceinline__ void lm_copy4(const void* g, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(g), "s"(to) : "memory");
+__device__ __forceinline__ void lm_copy4(const void* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory");
 }
 __device__ __forceinline__ void lm_copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -85,16 +86,27 @@ struct LmStream {
   static constexpr int IMG = kLmTile / 16 * L::G16, COPIES = kLmTile / L::RPC, NI = (COPIES + NW - 1) / NW;
   static_assert(COPIES >= 1, "a copy is at most a tile");
   static __device__ __forceinline__ int image_place(int c) { return D < 32 ? c * 1024 : (c * L::RPC >> 4) * L::G16 + (c * L::RPC & 15) / L::RPC * L::COPY; }
-  // src: row 0 of the tensor (bf16), ld elements per row; tile rows t0 .. t0 + 63 of `rows` (past the end: the last row)
-  static __device__ __forceinline__ void issue_one(const uint16_t* src, int ld, int t0, int rows, uint32_t buf, int lane, int wave) {
-    const char* base = reinterpret_cast<const char*>(src + (long long)t0 * ld);
-    const int last = rows - 1 - t0;
+  uint32_t off[NI];                // the lane's pieces of a whole tile, bytes from its first row
+  int ld;                          // elements per row
+  __device__ __forceinline__ LmStream(int ld_, int lane, int wave) : ld(ld_) {
 #pragma unroll
-    for (int n = 0; n < NI; ++n) {
-      const int c = wave + n * NW;                          // (the same for the wavefront)
-      if (COPIES % NW && c >= COPIES) break;
-      const int row = c * L::RPC + lane / L::CH, ch = (lane % L::CH) ^ L::swz(row);
-      lm_copy16(base + (uint32_t)(min(row, last) * ld) * 2u + 16 * ch, buf + image_place(c));
+    for (int n = 0; n < NI; ++n) off[n] = piece(n, kLmTile, lane, wave);
+  }
+  __device__ __forceinline__ uint32_t piece(int n, int rows, int lane, int wave) const {
+    const int row = (wave + n * NW) * L::RPC + lane / L::CH, ch = (lane % L::CH) ^ L::swz(row);
+    return (uint32_t)(min(row, rows - 1) * ld) * 2u + 16 * ch;
+  }
+  // src: row 0 of the tensor (bf16); tile rows t0 .. t0 + 63 of `rows` (past the end: the last row)
+  __device__ __forceinline__ void issue(const uint16_t* src, int t0, int rows, uint32_t buf, int lane, int wave) const {
+    const uint16_t* base = src + (long long)t0 * ld;
+    if (rows - t0 >= kLmTile) {
+#pragma unroll
+      for (int n = 0; n < NI; ++n)
+        if (COPIES % NW == 0 || wave + n * NW < COPIES) lm_copy16(base, off[n], buf + image_place(wave + n * NW));
+    } else {
+#pragma unroll
+      for (int n = 0; n < NI; ++n)
+        if (COPIES % NW == 0 || wave + n * NW < COPIES) lm_copy16(base, piece(n, rows - t0, lane, wave), buf + image_place(wave + n * NW));
     }
   }
 };
