@@ -16,7 +16,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["sbp_api.hip", "sbp_sampler.hip", "sbp_gather.hip", "sbp_linear.hip", "sbp_linear_f32.hip", "sbp_dwconv.hip", "sbp_pointwise.hip", "sbp_attention.hip", "sbp_static.hip",
-           "sbp_lm_api.hip", "sbp_lm_attention.hip", "sbp_lm_norm.hip", "sbp_lm_embedding.hip",
+           "sbp_lm_api.hip", "sbp_lm_attention.hip", "sbp_lm_norm.hip", "sbp_lm_embedding.hip", "sbp_lm_attention_f32.hip",
            *[f"sbp_lm_attention_{way}_{d}.hip" for way in ("fwd", "bwd") for d in (16, 32, 64, 128)]]
 LIB = os.path.join(HERE, "libsbp.so")
 NATIVE = os.path.join(HERE, "_native.so")        # the binding of the calls of every step (host code, against torch's headers)

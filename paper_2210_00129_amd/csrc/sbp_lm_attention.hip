@@ -6,47 +6,13 @@
 namespace sbp {
 
 template <typename T>
-__global__ void __launch_bounds__(256) masked_forward_rows_kernel(MaskedAttention a) {
-  const int lane = threadIdx.x & 63, nb = (int)((a.rows + 31) / 32), unit = blockIdx.x, c = unit % nb, bh = unit / nb;
-  for (int i = threadIdx.x >> 6; i < 32; i += 4) {
-    const int t = c * 32 + i;
-    if (t < a.rows) lm_forward_row<T>(a, bh / a.h, bh % a.h, t, lane);
-  }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256) masked_backward_rows_kernel(MaskedAttention a) {
-  const int lane = threadIdx.x & 63, nb = (int)((a.rows + 31) / 32), nq = a.B * a.h * nb;
-  const bool key = (int)blockIdx.x >= nq;
-  const int unit = key ? blockIdx.x - nq : blockIdx.x, c = unit % nb, bh = unit / nb;
-  for (int i = threadIdx.x >> 6; i < 32; i += 4) {
-    const int t = c * 32 + i;
-    if (t >= a.rows) continue;
-    if (!key) {
-      lm_backward_query<T>(a, bh / a.h, bh % a.h, t, lane);
-    } else {
-      const int b = bh / a.hk, kv = bh % a.hk, g = a.h / a.hk;
-      float dk[2], dv[2];
-      lm_backward_key<T>(a, b, kv, kv * g, (kv + 1) * g, t, lane, dk, dv);
-      T* o = (T*)a.out + ((long long)b * a.rows + t) * ((long long)(a.h + 2 * a.hk) * a.d) + (long long)(a.h + kv) * a.d;
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (lane + 64 * e < a.d) {
-          lm_store(o + lane + 64 * e, dk[e]);
-          lm_store(o + (long long)a.hk * a.d + lane + 64 * e, dv[e]);
-        }
-    }
-  }
-}
-
-template <typename T>
 __global__ void __launch_bounds__(256) masked_prepare_kernel(MaskedAttention a, LmTables w) {
+  // a workgroup per tile and head (head h: positions and documents)
   const int tiles = w.npad / kLmTile, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long unit = (long long)blockIdx.x * 4 + wave;  // a wavefront per tile and head; head h: positions and documents
-  if (unit >= (long long)a.B * (a.h + 1) * tiles) return;
-  const int tile = (int)(unit % tiles), bh = (int)(unit / tiles), b = bh / (a.h + 1), head = bh % (a.h + 1), t = tile * kLmTile + lane;
+  const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / (a.h + 1), head = bh % (a.h + 1), t = tile * kLmTile + lane;
   const bool on = t < a.rows;
   if (head == a.h) {
+    if (wave) return;
     const int p = on ? lm_pos(a, b, t) : 0, d = on ? lm_doc(a, b, p) : -1;
     w.pos[(long long)b * w.npad + t] = on ? (float)p : NAN;
     w.doc[(long long)b * w.npad + t] = d;
@@ -67,18 +33,20 @@ __global__ void __launch_bounds__(256) masked_prepare_kernel(MaskedAttention a, 
   constexpr int N = 16 / sizeof(T);
   const int per = a.d / N, rows = 64 / per;
   const long long ld = (long long)a.h * a.d, row0 = (long long)b * a.rows, at = ((long long)b * a.h + head) * w.npad + tile * kLmTile;
-  for (int r0 = 0; r0 < kLmTile; r0 += rows) {
+  for (int r0 = 16 * wave; r0 < 16 * wave + 16; r0 += rows) {
     const int row = r0 + lane / per, tok = tile * kLmTile + row, c = lane % per * N;
     float s = 0.f;
-    if (tok < a.rows) s = lm_dot((const T*)a.dA + (row0 + tok) * ld + head * a.d + c, (const T*)a.A + (row0 + tok) * ld + head * a.d + c, N);
+    if (row < 16 * wave + 16 && tok < a.rows) s = lm_dot((const T*)a.dA + (row0 + tok) * ld + head * a.d + c, (const T*)a.A + (row0 + tok) * ld + head * a.d + c, N);
     for (int m = 1; m < per; m <<= 1) s += __shfl_xor(s, m);
-    if (lane % per == 0) w.nd[at + row] = -s;
+    if (row < 16 * wave + 16 && lane % per == 0) w.nd[at + row] = -s;
   }
+  if (wave) return;
   const float l = on ? a.lse[(row0 + t) * a.h + head] : -INFINITY;
-  w.l2[at + lane] = l == -INFINITY ? 1e30f : l * kLog2e;    // (a weight of exp2(score - 1e30) = 0)
+  w.l2[at + lane] = l == -INFINITY ? 1e30f : l * (sizeof(T) == 2 ? kLog2e : 1.f);      // (a weight of exp(score - 1e30) = 0)
 }
 
 // Adds the parts of dK and dV of shared heads in order and rounds once: four channels per thread.
+template <typename T>
 __global__ void __launch_bounds__(256) masked_join_kernel(MaskedAttention a, LmTables w) {
   const long long pieces = (long long)a.B * a.rows * a.hk * 2 * a.d / 4, i = (long long)blockIdx.x * 256 + threadIdx.x;
   if (i >= pieces) return;
@@ -89,12 +57,13 @@ __global__ void __launch_bounds__(256) masked_join_kernel(MaskedAttention a, LmT
   }
   const int c = (int)(i * 4 % (2 * a.d)), kv = (int)(i * 4 / (2 * a.d) % a.hk);
   const long long row = i * 4 / (2 * a.d) / a.hk, ld = (long long)(a.h + 2 * a.hk) * a.d;
-  const int col = c < a.d ? (a.h + kv) * a.d + c : (a.h + a.hk + kv) * a.d + c - a.d;
-  *reinterpret_cast<uint2*>((uint16_t*)a.out + row * ld + col) = make_uint2(bf16_pack(s.x, s.y), bf16_pack(s.z, s.w));
+  T* out = (T*)a.out + row * ld + (c < a.d ? (a.h + kv) * a.d + c : (a.h + a.hk + kv) * a.d + c - a.d);
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pack(s.x, s.y), bf16_pack(s.z, s.w));
+  else *reinterpret_cast<float4*>(out) = s;
 }
 
-// Parts of a key / value head: its query heads follow one another in one workgroup per 128 keys unless that leaves fewer than two
-// workgroups per CU (256 CUs); then they are dealt to the smallest number of parts that does, each one more set of fp32 dK and dV.
+// Parts of a key / value head: its query heads follow one another in one workgroup per 128 keys (fp32: 32) unless that leaves fewer than
+// two workgroups per CU (256 CUs); then they are dealt to the smallest number of parts that does, each one more set of fp32 dK and dV.
 static int masked_parts(int64_t heads, int share, int nchunks) {
   int p = 1;
   while (p < share && heads * p * nchunks < 512) {
@@ -106,9 +75,9 @@ static int masked_parts(int64_t heads, int share, int nchunks) {
 
 MaskedAttentionPlan plan_masked_attention_backward(const sbp_attention_desc& d, int32_t n_k, int32_t dtype) {
   MaskedAttentionPlan p = {};
-  if (n_k == 0 || dtype != SBP_BF16) return p;
+  if (n_k == 0) return p;
   p.npad = (int)(ceil_div(n_k, kLmTile) * kLmTile);
-  p.nchunks = (int)ceil_div(n_k, kLmChunk);
+  p.nchunks = (int)ceil_div(n_k, dtype == SBP_BF16 ? kLmChunk : 32);
   p.parts = masked_parts((int64_t)d.B * d.h_kv, d.h / d.h_kv, p.nchunks);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
@@ -123,34 +92,31 @@ MaskedAttentionPlan plan_masked_attention_backward(const sbp_attention_desc& d, 
 }
 
 int32_t launch_forward_attention_masked(const MaskedAttention& a, int32_t dtype, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.h * ceil_div(a.rows, 32)));
-  if (dtype == SBP_BF16) {
-    if (a.d == 16) launch_masked_forward_bf16<16>(a, s);
-    else if (a.d == 32) launch_masked_forward_bf16<32>(a, s);
-    else if (a.d == 64) launch_masked_forward_bf16<64>(a, s);
-    else launch_masked_forward_bf16<128>(a, s);
-  } else SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_forward_rows_kernel<float>), grid, dim3(256), 0, s, a);
+  if (dtype != SBP_BF16) launch_masked_f32(a, nullptr, s);
+  else if (a.d == 16) launch_masked_forward_bf16<16>(a, s);
+  else if (a.d == 32) launch_masked_forward_bf16<32>(a, s);
+  else if (a.d == 64) launch_masked_forward_bf16<64>(a, s);
+  else launch_masked_forward_bf16<128>(a, s);
   return check_launch("forward_attention_masked");
 }
 
 int32_t launch_backward_attention_masked(const MaskedAttention& a, const MaskedAttentionPlan& p, int32_t dtype, void* ws_, hipStream_t s) {
-  if (dtype == SBP_BF16) {
-    char* ws = (char*)ws_;
-    const LmTables w{(float*)(ws + p.off_l2), (float*)(ws + p.off_nd), (float*)(ws + p.off_pos), (int32_t*)(ws + p.off_doc), (int4*)(ws + p.off_range),
-                     p.parts > 1 ? (float*)(ws + p.off_part) : nullptr, p.npad, p.parts, p.nchunks};
-    const int64_t units = (int64_t)a.B * (a.h + 1) * (p.npad / kLmTile);
-    SBP_LAUNCH(SBP_PROF_OTHER, s, (masked_prepare_kernel<uint16_t>), dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, s, a, w);
-    if (a.d == 16) launch_masked_backward_bf16<16>(a, w, s);
-    else if (a.d == 32) launch_masked_backward_bf16<32>(a, w, s);
-    else if (a.d == 64) launch_masked_backward_bf16<64>(a, w, s);
-    else launch_masked_backward_bf16<128>(a, w, s);
-    if (p.parts > 1) {
-      const int64_t pieces = (int64_t)a.B * a.rows * a.hk * 2 * a.d / 4;
-      SBP_LAUNCH(SBP_PROF_REDUCE, s, masked_join_kernel, dim3((unsigned)ceil_div(pieces, 256)), dim3(256), 0, s, a, w);
-    }
-  } else {
-    const dim3 grid((unsigned)((int64_t)a.B * (a.h + a.hk) * ceil_div(a.rows, 32)));
-    SBP_LAUNCH(SBP_PROF_ATTENTION, s, (masked_backward_rows_kernel<float>), grid, dim3(256), 0, s, a);
+  char* ws = (char*)ws_;
+  const bool bf16 = dtype == SBP_BF16;
+  const LmTables w{(float*)(ws + p.off_l2), (float*)(ws + p.off_nd), (float*)(ws + p.off_pos), (int32_t*)(ws + p.off_doc), (int4*)(ws + p.off_range),
+                   p.parts > 1 ? (float*)(ws + p.off_part) : nullptr, p.npad, p.parts, p.nchunks};
+  const dim3 prepare((unsigned)((int64_t)a.B * (a.h + 1) * (p.npad / kLmTile)));
+  if (bf16) SBP_LAUNCH(SBP_PROF_OTHER, s, (masked_prepare_kernel<uint16_t>), prepare, dim3(256), 0, s, a, w);
+  else SBP_LAUNCH(SBP_PROF_OTHER, s, (masked_prepare_kernel<float>), prepare, dim3(256), 0, s, a, w);
+  if (!bf16) launch_masked_f32(a, &w, s);
+  else if (a.d == 16) launch_masked_backward_bf16<16>(a, w, s);
+  else if (a.d == 32) launch_masked_backward_bf16<32>(a, w, s);
+  else if (a.d == 64) launch_masked_backward_bf16<64>(a, w, s);
+  else launch_masked_backward_bf16<128>(a, w, s);
+  if (p.parts > 1) {
+    const dim3 join((unsigned)ceil_div((int64_t)a.B * a.rows * a.hk * 2 * a.d / 4, 256));
+    if (bf16) SBP_LAUNCH(SBP_PROF_REDUCE, s, (masked_join_kernel<uint16_t>), join, dim3(256), 0, s, a, w);
+    else SBP_LAUNCH(SBP_PROF_REDUCE, s, (masked_join_kernel<float>), join, dim3(256), 0, s, a, w);
   }
   return check_launch("backward_attention_masked");
 }

@@ -30,6 +30,7 @@ struct LmTables;
 MaskedAttentionPlan plan_masked_attention_backward(const sbp_attention_desc& a, int32_t n_k, int32_t dtype);
 template <int D> void launch_masked_forward_bf16(const MaskedAttention& a, hipStream_t s);
 template <int D> void launch_masked_backward_bf16(const MaskedAttention& a, const LmTables& w, hipStream_t s);
+void launch_masked_f32(const MaskedAttention& a, const LmTables* w, hipStream_t s);        // w: backward
 int32_t launch_forward_attention_masked(const MaskedAttention& a, int32_t dtype, hipStream_t s);
 int32_t launch_backward_attention_masked(const MaskedAttention& a, const MaskedAttentionPlan& p, int32_t dtype, void* ws, hipStream_t s);
 
