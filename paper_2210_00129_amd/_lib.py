@@ -11,6 +11,7 @@ import os
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsbp.so")
 NATIVE_PATH = os.path.join(HERE, "_native.so")
+NATIVE_LM_PATH = os.path.join(HERE, "_native_lm.so")
 
 c_i32, c_i64, c_u32, c_u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64
 c_vp, c_sz, c_dbl = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_double
@@ -142,24 +143,41 @@ def check(status: int) -> int:
 
 
 _native = None
+_native_lm = None
+
+
+def _load(name, path):
+    import importlib.machinery
+    import importlib.util
+    if not os.path.exists(path):
+        raise RuntimeError(f"{path} is missing: build it with `python -m paper_2210_00129_amd.build`")
+    loader = importlib.machinery.ExtensionFileLoader(name, path)
+    m = importlib.util.module_from_spec(importlib.util.spec_from_file_location(name, path, loader=loader))
+    loader.exec_module(m)
+    return m
+
+
+def _bind(m, *names):
+    import torch
+    # (a torch without GPU support has no stream to ask for)
+    m.bind(*[ctypes.cast(getattr(lib(), n), ctypes.c_void_p).value for n in names], check, getattr(torch._C, "_cuda_getCurrentRawStream", None))
+    return m
 
 
 def native():
     """The native binding of the calls of every step (csrc/sbp_binding.cpp), bound to the loaded library."""
     global _native
     if _native is None:
-        import importlib.machinery
-        import importlib.util
-        import torch
-        L = lib()
-        if not os.path.exists(NATIVE_PATH):
-            raise RuntimeError(f"{NATIVE_PATH} is missing: build it with `python -m paper_2210_00129_amd.build`")
-        loader = importlib.machinery.ExtensionFileLoader("_native", NATIVE_PATH)
-        m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_native", NATIVE_PATH, loader=loader))
-        loader.exec_module(m)
-        names = ("sbp_keep_count", "sbp_sample_indices", "sbp_forward_cache", "sbp_backward_linear_workspace", "sbp_backward_linear")
-        # (a torch without GPU support has no stream to ask for)
-        m.bind(*[ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names], check,
-               getattr(torch._C, "_cuda_getCurrentRawStream", None))
-        _native = m
+        lib()
+        _native = _bind(_load("_native", NATIVE_PATH), "sbp_keep_count", "sbp_sample_indices", "sbp_forward_cache",
+                        "sbp_backward_linear_workspace", "sbp_backward_linear")
     return _native
+
+
+def native_lm():
+    """The native binding of the language-model steps (csrc/sbp_lm_binding.cpp), bound to the loaded library."""
+    global _native_lm
+    if _native_lm is None:
+        lib()
+        _native_lm = _bind(_load("_native_lm", NATIVE_LM_PATH), *LM_PROTOTYPES)
+    return _native_lm

@@ -20,6 +20,8 @@ SOURCES = ["sbp_api.hip", "sbp_sampler.hip", "sbp_gather.hip", "sbp_linear.hip",
            *[f"sbp_lm_attention_{way}_{d}.hip" for way in ("fwd", "bwd") for d in (16, 32, 64, 128)]]
 LIB = os.path.join(HERE, "libsbp.so")
 NATIVE = os.path.join(HERE, "_native.so")        # the binding of the calls of every step (host code, against torch's headers)
+NATIVE_LM = os.path.join(HERE, "_native_lm.so")  # ... of the language-model steps
+BINDINGS = {NATIVE: "sbp_binding.cpp", NATIVE_LM: "sbp_lm_binding.cpp"}
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -35,7 +37,7 @@ def hipcc() -> str:
     return exe
 
 
-def build_native() -> subprocess.Popen:
+def build_native(target: str) -> subprocess.Popen:
     import torch
     t = os.path.dirname(torch.__file__)
     inc = [os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
@@ -44,7 +46,7 @@ def build_native() -> subprocess.Popen:
     if cxx is None:
         raise RuntimeError("g++ not found")
     cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           *["-I" + i for i in inc], os.path.join(HERE, "csrc", "sbp_binding.cpp"), "-o", NATIVE + ".tmp",
+           *["-I" + i for i in inc], os.path.join(HERE, "csrc", BINDINGS[target]), "-o", target + ".tmp",
            "-L" + os.path.join(t, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath," + os.path.join(t, "lib")]
     return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
 
@@ -60,7 +62,7 @@ def build(verbose: bool = True) -> str:
         cmd = [hipcc(), *HIPCC_FLAGS, *inc, "-c", os.path.join(HERE, "csrc", src), "-o", obj]
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
-    native = build_native()
+    natives = {t: build_native(t) for t in BINDINGS}
     for src, p in procs:
         out, _ = p.communicate()
         out = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
@@ -73,11 +75,13 @@ def build(verbose: bool = True) -> str:
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stdout)
-    out, _ = native.communicate()
-    if native.returncode != 0:
-        raise RuntimeError("g++ failed on sbp_binding.cpp:\n" + out)
+    for target, p in natives.items():
+        out, _ = p.communicate()
+        if p.returncode != 0:
+            raise RuntimeError(f"g++ failed on {BINDINGS[target]}:\n" + out)
     os.replace(tmp, LIB)
-    os.replace(NATIVE + ".tmp", NATIVE)
+    for target in natives:
+        os.replace(target + ".tmp", target)
     if verbose:
         print("built", LIB)
     return LIB
