@@ -42,7 +42,7 @@ typedef struct sbp_attention_desc {
   int32_t  d;             /* head dimension: 16, 32, 64 or 128 */
   int32_t  causal;        /* 0 or 1 */
   float    scale;         /* usually 1 / sqrt(d); finite */
-  float    cap;           /* >= 0, finite; 0: scores are not capped */
+  float    cap;           /* 0 .. 1024; 0: scores are not capped */
   const float*   slopes;  /* device, [h] fp32, or NULL */
   const int32_t* doc;     /* device, [B*n] document of every token (any numbers; < 0: of none), or NULL */
   const int32_t* prefix;  /* device, [B] keys at positions below it are visible to all queries of the sample (within the
@@ -55,7 +55,7 @@ typedef struct sbp_attention_desc {
  *        sbp_backward_attention)
  *   A    device, out, [B*n, h*d] of `dtype`
  *   lse  device, out, [B*n, h] fp32, natural logarithm; or NULL
- * qkv and A 16-byte aligned.  Sums and the softmax statistics are fp32; in bf16 the probabilities are rounded to bf16
+ * qkv and A 16-byte aligned, A not qkv.  Sums and the softmax statistics are fp32; in bf16 the probabilities are rounded to bf16
  * before the second product.  Deterministic.
  */
 int32_t sbp_forward_attention_masked(const sbp_attention_desc* desc, const void* qkv, int32_t dtype, void* A, float* lse,
@@ -167,7 +167,7 @@ size_t sbp_backward_embedding_workspace(int64_t M, int64_t K, int64_t V, int32_t
  *           also the output projection's weight)
  *   flags   SBP_FLAG_DY_COMPACT, SBP_FLAG_ACCUMULATE_DW, SBP_FLAG_DW_OUT_BF16
  *   workspace  device, 256-byte aligned, sbp_backward_embedding_workspace(...) bytes
- * K < 2^30, V < 2^30.
+ * K < 2^30, V < 2^30, K * C < 2^37.
  */
 int32_t sbp_backward_embedding(const void* dE, const void* tokens, int32_t token_bytes, const int32_t* idx, int64_t M, int64_t K,
                                int64_t V, int32_t C, float scale, int32_t dtype, void* dtable, void* workspace,

@@ -53,7 +53,7 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
   const uint16_t* dA = (const uint16_t*)a.dA + row0 * lda;
   const int first = chunk * kLmChunk + wave * 32, mine = first + (lane & 31), own = min(mine, rows - 1);
   const bool busy = first < rows, docs = a.doc != nullptr;
-  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const int prefix = lm_prefix(a, b);
   const L lay(lane);
   const uint32_t lds0 = lm_lds(smem);
   const typename F::S st1(ld, lane, wave), st2(lda, lane, wave);

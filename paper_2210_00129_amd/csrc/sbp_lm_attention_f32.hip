@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(256) masked_forward_f32_kernel(MaskedAttention
   const float *k0 = base + (a.h + kv) * D, *v0 = k0 + a.hk * D;
   const bool docs = a.doc != nullptr;
   const int32_t* doc = docs ? a.doc + (long long)b * n : nullptr;
-  const int prefix = a.prefix ? a.prefix[b] : 0, di = docs ? doc[own] : 0;
+  const int prefix = lm_prefix(a, b), di = docs ? doc[own] : 0;
   const float slope = a.slopes ? a.slopes[head] : 0.f;
   LmRange wq{first, min(first + 31, n - 1), 0, 0};
   if (docs) {
@@ -208,7 +208,7 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
   const float *qkv = (const float*)a.qkv + row0 * ld, *dA = (const float*)a.dA + row0 * lda;
   const int first = blk * 32, mine = first + (lane & 31), own = min(mine, rows - 1), blocks = (rows + 31) / 32, tiles = w.npad / kLmTile;
   const bool docs = a.doc != nullptr;
-  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const int prefix = lm_prefix(a, b);
   const float own_pos = w.pos[(long long)b * w.npad + own];
   const int own_doc = w.doc[(long long)b * w.npad + own];
   float bound = KEY ? -3e38f : 3e38f;                       // streamed positions >= bound (KEY) or <= bound are visible

@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
   const int first = chunk * 32 * NW + wave * 32, mine = first + (lane & 31), own = min(mine, n - 1);
   const bool busy = first < n;
   const bool docs = a.doc != nullptr;
-  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const int prefix = lm_prefix(a, b);
   const int32_t* doc = docs ? a.doc + (long long)b * n : nullptr;
   const int di = docs ? doc[own] : 0;
   const L lay(lane);
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
       }
       if (s > 0 && s <= ns) st.issue(v0, (base_tile + before) * kLmTile, n, buf + F::S::IMG, lane, wave);
     };
-        int copied = __builtin_amdgcn_readfirstlane(entry(0).x), coming = __builtin_amdgcn_readfirstlane(entry(1).x);
+    int copied = __builtin_amdgcn_readfirstlane(entry(0).x), coming = __builtin_amdgcn_readfirstlane(entry(1).x);
     issue(0, copied, 0);
     const bool late = PAIR && wave >= NW / 2;                // this wavefront runs half a stage behind
     // the meeting before stage s: its copies have arrived everywhere, the places of stage s - 1 are free; and the one half a stage later
@@ -357,8 +357,13 @@ static void launch_masked_forward_mode(const MaskedAttention& a, hipStream_t s) 
 }
 template <int D>
 void launch_masked_forward_bf16(const MaskedAttention& a, hipStream_t s) {
-  if (a.n > (D == 128 ? 128 : 1 << 30)) launch_masked_forward_mode<D, 8>(a, s);
-  else launch_masked_forward_mode<D, 4>(a, s);
+  // Pairs of wavefronts half a stage apart pay where the products of a stage are many (d = 128: the long text 314 us, with 4 wavefronts
+  // 398) and there is more than one workgroup of 4 to a head; for smaller d the meetings cost more than they hide (4 x 12 heads of 64,
+  // 2048 packed tokens: 62 us with 4 wavefronts, 80 with 8; 16 samples of them 163 and 218).
+  if constexpr (D == 128) {
+    if (a.n > 128) return launch_masked_forward_mode<D, 8>(a, s);
+  }
+  launch_masked_forward_mode<D, 4>(a, s);
 }
 
 }  // namespace sbp

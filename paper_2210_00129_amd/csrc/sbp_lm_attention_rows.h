@@ -45,6 +45,8 @@ __device__ __forceinline__ float lm_wave_max(float v) {
 // where token t of sample b stands, and the document it belongs to
 __device__ __forceinline__ int lm_pos(const MaskedAttention& a, int b, int t) { return a.idx ? a.idx[(long long)b * a.rows + t] - b * a.n : t; }
 __device__ __forceinline__ int lm_doc(const MaskedAttention& a, int b, int pos) { return a.doc ? a.doc[(long long)b * a.n + pos] : 0; }
+// (no position is below 0: differences of prefix and a position stay within 32 bits)
+__device__ __forceinline__ int lm_prefix(const MaskedAttention& a, int b) { return a.prefix ? max(a.prefix[b], 0) : 0; }
 __device__ __forceinline__ bool lm_visible(const MaskedAttention& a, int prefix, int pi, int di, int pj, int dj) {
   return (!a.causal || pj <= pi || pj < prefix) && di == dj && di >= 0;
 }
@@ -64,7 +66,7 @@ __device__ void lm_forward_row(const MaskedAttention& a, int b, int head, int t,
   const T* q = (const T*)a.qkv + (row0 + t) * ld + head * d;
   const T* k = (const T*)a.qkv + row0 * ld + (long long)(a.h + kv) * d;
   const T* v = k + (long long)a.hk * d;
-  const int prefix = a.prefix ? a.prefix[b] : 0, pi = lm_pos(a, b, t), di = lm_doc(a, b, pi);
+  const int prefix = lm_prefix(a, b), pi = lm_pos(a, b, t), di = lm_doc(a, b, pi);
   const float slope = a.slopes ? a.slopes[head] : 0.f;
   float m = -INFINITY, l = 0.f, acc0 = 0.f, acc1 = 0.f;
   for (int j0 = 0; j0 < a.rows; j0 += 64) {
@@ -118,7 +120,7 @@ __device__ void lm_backward_query(const MaskedAttention& a, int b, int head, int
   const T* o = (const T*)a.A + (row0 + t) * lda + head * d;
   const T* k = (const T*)a.qkv + row0 * ld + (long long)(a.h + kv) * d;
   const T* v = k + (long long)a.hk * d;
-  const int prefix = a.prefix ? a.prefix[b] : 0, pi = lm_pos(a, b, t), di = lm_doc(a, b, pi);
+  const int prefix = lm_prefix(a, b), pi = lm_pos(a, b, t), di = lm_doc(a, b, pi);
   const float slope = a.slopes ? a.slopes[head] : 0.f, delta = lm_dot(g, o, d), lse = a.lse[(row0 + t) * a.h + head];
   float acc0 = 0.f, acc1 = 0.f;
   for (int j0 = 0; j0 < a.rows; j0 += 64) {
@@ -150,7 +152,7 @@ __device__ void lm_backward_key(const MaskedAttention& a, int b, int kv, int h0,
   const long long ld = (long long)(a.h + 2 * a.hk) * d, lda = (long long)a.h * d, row0 = (long long)b * a.rows;
   const T* k = (const T*)a.qkv + (row0 + t) * ld + (long long)(a.h + kv) * d;
   const T* v = k + (long long)a.hk * d;
-  const int prefix = a.prefix ? a.prefix[b] : 0, pj = lm_pos(a, b, t), dj = lm_doc(a, b, pj);
+  const int prefix = lm_prefix(a, b), pj = lm_pos(a, b, t), dj = lm_doc(a, b, pj);
   dk[0] = dk[1] = dv[0] = dv[1] = 0.f;
   for (int head = h0; head < h1; ++head) {
     const T* q = (const T*)a.qkv + row0 * ld + head * d;

@@ -256,3 +256,18 @@ def test_the_binding_refuses_what_does_not_fit():
                       (lambda: sbp.forward_attention_masked(torch.zeros(8, 192, device="cuda")[:, ::2], 2, 2, 16, 0.25), ValueError)]:
         with pytest.raises(err):
             call()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 128])
+def test_prefix_beyond_the_sample(dtype, d):
+    c = Case(4, 197, 2, 1, d, dtype, seed=21, causal=True, prefix=[-2 ** 31, -1, 2 ** 31 - 1, 197])
+    check_forward(c)
+    check_backward(c, _keep(4, 197, 120, 21))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_largest_cap(dtype):
+    c = Case(1, 150, 2, 1, 64, dtype, seed=22, causal=True, cap=1024.0, spread=3.0)
+    check_forward(c)
+    check_backward(c, _keep(1, 150, 90, 22))

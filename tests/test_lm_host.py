@@ -164,3 +164,19 @@ def test_binding_refuses_host_tensors():
             call()
     with pytest.raises(ValueError, match="one of"):
         sbp.backward_residual_norm(None, None, None, None, i, 4)
+
+
+def test_attention_refuses_what_its_kernels_cannot_hold():
+    L = _lib.lib()
+    assert L.sbp_forward_attention_masked(_attn(cap=1025.0), P, 1, 2 * P, P, None) == SHAPE      # tanh to a few steps of fp32 of the cap
+    assert L.sbp_backward_attention_masked_workspace(_attn(cap=1025.0), 5, 1) == 0
+    assert L.sbp_backward_attention_masked_workspace(_attn(cap=1024.0), 5, 1) > 0
+    assert L.sbp_forward_attention_masked(_attn(), P, 1, P, P, None) == SHAPE                    # the output is the input
+
+
+def test_table_gradient_refuses_more_units_than_a_grid_has():
+    L = _lib.lib()
+    K, C = 1 << 25, 1 << 13
+    assert L.sbp_backward_embedding_workspace(K, K, 1000, C, 1, 0) == 0
+    assert L.sbp_backward_embedding(P, P, 4, None, K, K, 1000, C, 1.0, 1, P, 4 * P, 1 << 60, 0, None) == SHAPE
+    assert L.sbp_backward_embedding_workspace(K, K - 32, 1000, C // 2, 1, 0) > 0
