@@ -32,6 +32,14 @@ static constexpr float kLmSlack = 6.f, kLmFixedCap = 60.f;
 static constexpr int kLmAhead = 6;
 static constexpr int kLmList = 128;                        // tiles per list (8192 tokens); longer samples take several
 
+// max(a, b, c); of the numbers where some are NaN.  (fmaxf() first makes every operand that the compiler does not know to be a quiet
+// one quiet, which doubles the steps.)  The operands must not be results of a matrix instruction under way.
+__device__ __forceinline__ float lm_max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 template <int D, int NW>
 struct LmFwd {
   using L = AttnSwizzled<D>;
@@ -46,7 +54,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
   using L = AttnSwizzled<D>;
   using F = LmFwd<D, NW>;
   constexpr int KS = L::KS, DB = L::DB;
-  constexpr bool PAIR = NW == 8;
+  constexpr bool PAIR = NW == 8, CAP = MODE == LM_CAP || MODE == LM_CAP_FIXED, BIAS = MODE == LM_CAP || MODE == LM_BIAS;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int4 list_s[kLmList];                           // a tile to look at, the documents in it
   __shared__ int range_s[2 * NW + 1];
@@ -64,6 +72,10 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
   const int prefix = lm_prefix(a, b);
   const int32_t* doc = docs ? a.doc + (long long)b * n : nullptr;
   const int di = docs ? doc[own] : 0;
+  int dv[4] = {0, 0, 0, 0};                                 // documents of four tokens of tile t / 16, for the first list
+  if (docs)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dv[e] = doc[min((t >> 4) * kLmTile + (t & 15) * 4 + e, n - 1)];
   const L lay(lane);
   const uint32_t lds0 = lm_lds(smem);
   const typename F::S st(ld, lane, wave);
@@ -84,6 +96,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
     wq.d0 = __builtin_amdgcn_readfirstlane(r.lo);
     wq.d1 = __builtin_amdgcn_readfirstlane(r.hi);
   }
+  const bool strays = __ballot(di < 0) != 0;                // queries of no document
   LmRange gq;                                               // ... of the workgroup's
   gq.p0 = chunk * 32 * NW; gq.p1 = min(gq.p0 + 32 * NW - 1, n - 1); gq.d0 = gq.d1 = 0;
   if (docs) {
@@ -93,8 +106,15 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
 #pragma unroll
     for (int w = 1; w < NW; ++w) { gq.d0 = min(gq.d0, range_s[w]); gq.d1 = max(gq.d1, range_s[NW + w]); }
   }
-  const float slope2 = (MODE == LM_BIAS || MODE == LM_CAP) && a.slopes ? a.slopes[head] * kLog2e : 0.f;
-  const float c2 = a.scale * kLog2e, cap2 = a.cap * kLog2e, ct = MODE >= LM_CAP_FIXED ? 2.f * kLog2e * a.scale / a.cap : 0.f;
+  const float slope2 = BIAS && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+  float c2 = a.scale * kLog2e;
+  if constexpr (BIAS) asm("" : "+v"(c2));                    // (a fused product reads one scalar register: the bias)
+  const float cap2 = a.cap * kLog2e, ct = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f;
+  float ahead[BIAS ? 16 : 1];                                // bias of a block's keys relative to the lane's first one (wave-uniform: scalar registers)
+  if constexpr (BIAS)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ahead[e] = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(slope2 * (float)(8 * (e >> 2) + (e & 3)))));
+  const bool forward_only = a.causal && prefix == 0;         // no visible key stands behind its query
 
   f32x16_t o[DB];
 #pragma unroll
@@ -131,49 +151,83 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
   };
   using Yes = std::true_type;
   using No = std::false_type;
-  // scores of the tile at position p into weights; td: the documents of its keys
-  auto weigh = [&](bool masked, const int* td, int p) {
-    const int rel = mine - p - 4 * u;                        // distance to the lane's key of register 0
-    const float relf = (float)rel;
+  // Scores of a tile into weights; r: its positions and documents, td: the documents of its keys.
+  // Bias: where no visible key stands behind its query, slope |pos_i - pos_j| is linear, and what the lane's keys have in common of it
+  // joins the maximum's subtraction.
+  auto weigh = [&](const LmRange& r, const int* td) {
+    const int p = r.p0, rel = mine - p - 4 * u;              // rel: distance to the lane's key of register 0
+    float common[2] = {0.f, 0.f};
     if constexpr (MODE != LM_PLAIN) {
+      const float relf = (float)rel;
+      const bool linear = BIAS && (forward_only || r.p1 <= wq.p0);
+      if (linear) {
+        common[0] = -slope2 * relf;
+        common[1] = -slope2 * (relf - 32.f);
+      }
+      if constexpr (CAP) {
+        // cap tanh(z / cap) by one exponential and a reciprocal (a polynomial for small arguments has more steps than these: the long text
+        // 372 us instead of 313)
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+        for (int y = 0; y < 2; ++y)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float v = sc[y][e];
-          if constexpr (MODE == LM_BIAS) v *= c2;
-          else v = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(v * ct) + 1.f), cap2);   // cap tanh(z / cap)
-          if constexpr (MODE != LM_CAP_FIXED) v = fmaf(-slope2, fabsf(relf - (float)(32 * y + 8 * (e >> 2) + (e & 3))), v);
-          sc[y][e] = v;
+          for (int e = 0; e < 16; ++e) sc[y][e] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(sc[y][e] * ct) + 1.f), cap2);
+      }
+      if constexpr (BIAS) {
+        if (linear) {
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              if constexpr (CAP) sc[y][e] += ahead[e];
+              else sc[y][e] = fmaf(sc[y][e], c2, ahead[e]);
+            }
+        } else {
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float v = CAP ? sc[y][e] : sc[y][e] * c2;
+              sc[y][e] = fmaf(-slope2, fabsf(relf - (float)(32 * y + 8 * (e >> 2) + (e & 3))), v);
+            }
         }
+      }
     }
-    if (masked) {
+    // element by element only what the ranges leave open
+    if (r.p1 >= n || strays || (a.causal && r.p1 > wq.p0 && r.p1 >= prefix)) {
       // the lane's keys of registers with row < lim are seen: up to the query's own position or the end of the prefix, and of the sample
       int lim = n - p - 4 * u;
       if (a.causal) lim = min(lim, max(rel + 1, prefix - p - 4 * u));
-      if (docs && di < 0) lim = 0;
+      if (di < 0) lim = 0;
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[y][e] = 32 * y + 8 * (e >> 2) + (e & 3) < lim ? sc[y][e] : -INFINITY;
+    }
+    if (docs && !(r.d0 == r.d1 && wq.d0 == wq.d1 && r.d0 == wq.d0)) {
 #pragma unroll
       for (int y = 0; y < 2; ++y)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
-          int4 dj = make_int4(0, 0, 0, 0);
-          if (docs) dj = *reinterpret_cast<const int4*>(td + 32 * y + 4 * u + 8 * q4);
+          const int4 dj = *reinterpret_cast<const int4*>(td + 32 * y + 4 * u + 8 * q4);
           const int dk[4] = {dj.x, dj.y, dj.z, dj.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool see = 32 * y + 8 * q4 + e < lim && (!docs || dk[e] == di);
-            sc[y][4 * q4 + e] = see ? sc[y][4 * q4 + e] : -INFINITY;
-          }
+          for (int e = 0; e < 4; ++e) sc[y][4 * q4 + e] = dk[e] == di ? sc[y][4 * q4 + e] : -INFINITY;
         }
     }
     if constexpr (MODE != LM_CAP_FIXED) {
-      float mx = -INFINITY;
+      // (plain scores come from the matrix cores as they are: 24 cycles let the last product finish)
+      if constexpr (MODE == LM_PLAIN) asm volatile("s_nop 15\n\ts_nop 7" : "+v"(sc[0]), "+v"(sc[1]));
+      float top[2];
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+      for (int y = 0; y < 2; ++y) {
+        top[y] = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) mx = fmaxf(mx, fmaxf(sc[y][e], sc[y][e + 1]));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+        for (int e = 0; e < 16; e += 2) top[y] = lm_max3(top[y], sc[y][e], sc[y][e + 1]);
+        if constexpr (BIAS) top[y] += common[y];
+      }
+      float mx = fmaxf(top[0], top[1]);
       if constexpr (MODE == LM_PLAIN) mx *= c2;
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
       if (__ballot(mx > m2 + kLmSlack)) {
         const float mn = mx > m2 + kLmSlack ? mx : m2, f = mn > m2 ? __builtin_amdgcn_exp2f(m2 - mn) : 1.f;
         m2 = mn;
@@ -184,9 +238,9 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
           for (int e = 0; e < 16; ++e) o[x][e] *= f;
       }
     }
-    const float ms = m2 == -INFINITY ? 0.f : m2;             // (nothing seen so far: every weight is 0)
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
+      const float ms = (m2 == -INFINITY ? 0.f : m2) - (BIAS ? common[y] : 0.f);      // (nothing seen so far: every weight is 0)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         if constexpr (MODE == LM_PLAIN) sc[y][e] = __builtin_amdgcn_exp2f(fmaf(sc[y][e], c2, -ms));
@@ -211,11 +265,11 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
         const int i = i0 + (t >> 4), at = (base_tile + i) * kLmTile + (t & 15) * 4;
         LmDocs r;
         if (i < here) {
-          int v[4];
+          if (base_tile + i0)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = doc[min(at + e, n - 1)];
+            for (int e = 0; e < 4; ++e) dv[e] = doc[min(at + e, n - 1)];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) r.add(v[e]);
+          for (int e = 0; e < 4; ++e) r.add(dv[e]);
         }
 #pragma unroll
         for (int m = 1; m < 16; m <<= 1) r.join(m);
@@ -290,8 +344,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
       LmRange r;
       r.p0 = (base_tile + __builtin_amdgcn_readfirstlane(e.x)) * kLmTile; r.p1 = r.p0 + kLmTile - 1;
       r.d0 = __builtin_amdgcn_readfirstlane(e.y); r.d1 = __builtin_amdgcn_readfirstlane(e.z);
-      const bool masked = r.p1 >= n || lm_class(wq, r, a.causal, prefix, docs) != 2;
-      weigh(masked, reinterpret_cast<const int*>(smem + F::DOCS + (t & 3) * (4 * kLmTile)), r.p0);
+      weigh(r, reinterpret_cast<const int*>(smem + F::DOCS + (t & 3) * (4 * kLmTile)));
     };
     wait_async_copies<0>();                                  // (the queries' loads too, lest the loop waits for them)
     if (late) meet(true, 0);
