@@ -11,6 +11,7 @@
 namespace sbp {
 
 template <int D> struct LmF32 {
+  static constexpr int PITCH = D + 4;                      // of rows in LDS
   static constexpr int DB = D < 32 ? 1 : D / 32, W = D < 32 ? D : 32;      // blocks of head dimensions, dimensions of one
   // dimensions 8 c + 4 u .. + 3 of a row, in order
   static __device__ __forceinline__ void row(const float* p, int u, float (&v)[D / 2]) {
@@ -29,24 +30,36 @@ template <int D> struct LmF32 {
     for (int i = 0; i < D / 2; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(rows[i], own[i], s, 0, 0, 0);
     return s;
   }
-  // acc += block^T w: block: 32 rows from `base` on (ld elements apart, at most `last` rows on), w: register v belongs to row 8 (v >> 2) + 4 u + (v & 3)
-  static __device__ __forceinline__ void add(f32x16_t (&acc)[DB], const float* base, long long ld, int last, const f32x16_t& w, int lane) {
+  // ... with the own rows in LDS ([32][PITCH]: 16 bytes for four products)
+  static __device__ __forceinline__ f32x16_t scores(const float (&rows)[D / 2], const float* own, int lane) {
+    f32x16_t s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    const float* at = own + (lane & 31) * PITCH + 4 * (lane >> 5);
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(at + 8 * c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(rows[4 * c + e], x[e], s, 0, 0, 0);
+    }
+    return s;
+  }
+  // columns of a block: 32 rows from `base` on (ld elements apart, at most `last` rows on), register v of row 8 (v >> 2) + 4 u + (v & 3)
+  static __device__ __forceinline__ void columns(float (&x)[16][DB], const float* base, long long ld, int last, int lane) {
     const int u = lane >> 5, col = lane & (W - 1);
 #pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {
-      float x[4][DB];
+    for (int v = 0; v < 16; ++v)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int b = 0; b < DB; ++b) x[v][b] = base[min(8 * (v >> 2) + 4 * u + (v & 3), last) * ld + col + 32 * b];
+  }
+  // acc += block^T w
+  static __device__ __forceinline__ void add(f32x16_t (&acc)[DB], const float (&x)[16][DB], const f32x16_t& w) {
 #pragma unroll
-        for (int b = 0; b < DB; ++b) x[e][b] = base[min(8 * q4 + 4 * u + e, last) * ld + col + 32 * b];
+    for (int v = 0; v < 16; ++v)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int b = 0; b < DB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e][b], w[4 * q4 + e], acc[b], 0, 0, 0);
-    }
+      for (int b = 0; b < DB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[v][b], w[v], acc[b], 0, 0, 0);
   }
   // the wavefront's accumulators to LDS: [32 own tokens][D + 4]
-  static constexpr int PITCH = D + 4;
   static __device__ __forceinline__ void put(float* img, const f32x16_t (&acc)[DB], int lane) {
 #pragma unroll
     for (int b = 0; b < DB; ++b)
@@ -57,12 +70,20 @@ template <int D> struct LmF32 {
   }
 };
 
+// tanh to about a step of fp32, without branches: up to 0.55 an odd polynomial (of least largest error, 2^-29 of the value), beyond it
+// 1 - 2 / (exp(2 |x|) + 1).  (tanhf() takes both of its ways where the lanes differ.)
+__device__ __forceinline__ float lm_tanh(float x) {
+  const float u = x * x, y = fabsf(x);
+  const float near = fmaf(x * u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -0.0062824725f, 0.021077758f), -0.05385386f), 0.13332602f), -0.3333332f), x);
+  const float far = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.f * kLog2e)) + 1.f), 1.f);
+  return y > 0.55f ? copysignf(far, x) : near;
+}
 // the score (natural units) of z = q.k and, capped, the square of its tanh
 template <bool CAP>
-__device__ __forceinline__ float lm_score_f32(const MaskedAttention& a, float slope, float z, float distance, float* t2) {
+__device__ __forceinline__ float lm_score_f32(const MaskedAttention& a, float inv_cap, float slope, float z, float distance, float* t2) {
   float s = a.scale * z;
   if constexpr (CAP) {
-    const float t = tanhf(s / a.cap);
+    const float t = lm_tanh(s * inv_cap);
     *t2 = t * t;
     s = a.cap * t;
   }
@@ -84,7 +105,7 @@ __global__ void __launch_bounds__(256) masked_forward_f32_kernel(MaskedAttention
   const bool docs = a.doc != nullptr;
   const int32_t* doc = docs ? a.doc + (long long)b * n : nullptr;
   const int prefix = lm_prefix(a, b), di = docs ? doc[own] : 0;
-  const float slope = a.slopes ? a.slopes[head] : 0.f;
+  const float slope = a.slopes ? a.slopes[head] : 0.f, inv_cap = CAP ? 1.f / a.cap : 0.f;
   LmRange wq{first, min(first + 31, n - 1), 0, 0};
   if (docs) {
     LmDocs r;
@@ -123,12 +144,15 @@ __global__ void __launch_bounds__(256) masked_forward_f32_kernel(MaskedAttention
     float k[D / 2];
     F::row(k0 + min(j0 + (lane & 31), n - 1) * ld, u, k);
     f32x16_t s = F::scores(k, q);
+    float v[16][F::DB];                                      // (under way while the weights are worked out)
+    F::columns(v, v0 + j0 * ld, ld, n - 1 - j0, lane);
+    __builtin_amdgcn_sched_barrier(0);
     const int rel = mine - j0 - 4 * u;
     float top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       float unused;
-      s[e] = lm_score_f32<CAP>(a, slope, s[e], fabsf((float)(rel - (8 * (e >> 2) + (e & 3)))), &unused);
+      s[e] = lm_score_f32<CAP>(a, inv_cap, slope, s[e], fabsf((float)(rel - (8 * (e >> 2) + (e & 3)))), &unused);
     }
     if (cls != 2 || j0 + 31 >= n) {
       int lim = n - j0 - 4 * u;
@@ -159,7 +183,7 @@ __global__ void __launch_bounds__(256) masked_forward_f32_kernel(MaskedAttention
       s[e] = expf(s[e] - ms);
       l += s[e];
     }
-    F::add(o, v0 + j0 * ld, ld, n - 1 - j0, s, lane);
+    F::add(o, v, s);
   }
   // join the wavefronts: their maxima, sums and outputs
   l += __shfl_xor(l, 32);
@@ -219,10 +243,24 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
     own_l = w.l2[((long long)b * a.h + h0) * w.npad + own];
     own_nd = w.nd[((long long)b * a.h + h0) * w.npad + own];
   }
-  float f1[D / 2], f2[D / 2];                               // k, v (KEY) or q, dA of the own token
+  // k, v (KEY) or q, dA of the own tokens: in registers, or, where these are short (d = 128 with them: 105 registers in memory, 734 us
+  // for 13 x 2 heads, 1273 tokens in documents of 300; without 523), in LDS
+  constexpr bool OWN = D < 128;
+  float f1[OWN ? D / 2 : 1], f2[OWN ? D / 2 : 1];
   const float* p1 = qkv + own * ld + (KEY ? a.h + kv : h0) * D;
-  F::row(p1, u, f1);
-  F::row(KEY ? p1 + a.hk * D : dA + own * lda + h0 * D, u, f2);
+  const float* p2 = KEY ? p1 + a.hk * D : dA + own * lda + h0 * D;
+  if constexpr (OWN) {
+    F::row(p1, u, f1);
+    F::row(p2, u, f2);
+  } else {
+#pragma unroll
+    for (int c = D / 32 * wave; c < D / 32 * (wave + 1); ++c) {      // 8 dimensions each, a quarter per wavefront
+      float* at = img + (lane & 31) * F::PITCH + 8 * c + 4 * u;
+      *reinterpret_cast<float4*>(at) = *reinterpret_cast<const float4*>(p1 + 8 * c + 4 * u);
+      *reinterpret_cast<float4*>(at + 32 * F::PITCH) = *reinterpret_cast<const float4*>(p2 + 8 * c + 4 * u);
+    }
+    __syncthreads();
+  }
   f32x16_t acc[KEY ? 2 : 1][F::DB];
 #pragma unroll
   for (int q = 0; q < (KEY ? 2 : 1); ++q)
@@ -231,6 +269,7 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[q][x][e] = 0.f;
   if (t == 0) *again_s = 0;
+  const float inv_cap = CAP ? 1.f / a.cap : 0.f;
   const int4* ranges = w.range + (long long)b * tiles;
   const int4 mr4 = ranges[blk >> 1];
   const LmRange mr{mr4.x, mr4.y, mr4.z, mr4.w};
@@ -260,13 +299,23 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
       tp[q4] = *reinterpret_cast<const f32x4_t*>(w.pos + at);
       td[q4] = *reinterpret_cast<const int4*>(w.doc + at);
     }
-    f32x16_t s = F::scores(x1, f1), dp = F::scores(x2, f2);
+    f32x16_t s, dp;
+    if constexpr (OWN) {
+      s = F::scores(x1, f1);
+      dp = F::scores(x2, f2);
+    } else {
+      s = F::scores(x1, img, lane);
+      dp = F::scores(x2, img + 32 * F::PITCH, lane);
+    }
+    float c[16][F::DB];                                      // (under way while the weights are worked out)
+    F::columns(c, s1 + t0 * ld, ld, last, lane);
+    __builtin_amdgcn_sched_barrier(0);
     const bool masked = cls != 2 || last < 31;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int q4 = e >> 2, k = e & 3;
       float t2 = 0.f;
-      const float v = lm_score_f32<CAP>(a, slope, s[e], fabsf(tp[q4][k] - own_pos), &t2);
+      const float v = lm_score_f32<CAP>(a, inv_cap, slope, s[e], fabsf(tp[q4][k] - own_pos), &t2);
       float p = expf(v - (KEY ? tl[q4][k] : own_l)), m = p * (dp[e] + (KEY ? tn[q4][k] : own_nd)) * a.scale;
       if constexpr (CAP) m *= 1.f - t2;
       if (masked) {
@@ -278,8 +327,15 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
       s[e] = p;
       dp[e] = m;
     }
-    F::add(acc[0], s1 + t0 * ld, ld, last, dp, lane);
-    if constexpr (KEY) F::add(acc[1], s2 + t0 * ld2, ld2, last, s, lane);
+    if constexpr (KEY) {
+      float c2[16][F::DB];                                   // (under way while the first products run)
+      F::columns(c2, s2 + t0 * ld2, ld2, last, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      F::add(acc[0], c, dp);
+      F::add(acc[1], c2, s);
+    } else {
+      F::add(acc[0], c, dp);
+    }
   }
   // join the wavefronts' sums in order
   float* out = (float*)a.out + row0 * ld;
@@ -326,7 +382,7 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
 }
 
 template <int D, bool CAP>
-__global__ void __launch_bounds__(256) masked_backward_f32_kernel(MaskedAttention a, LmTables w) {
+__global__ void __launch_bounds__(256, D <= 32 ? 2 : 1) masked_backward_f32_kernel(MaskedAttention a, LmTables w) {
   __shared__ __attribute__((aligned(16))) float img[4 * 32 * LmF32<D>::PITCH];
   __shared__ uint32_t again_s;
   const int nk = a.B * a.hk * w.parts, nq = a.B * a.h, blocks = (a.rows + 31) / 32, rank = blockIdx.x / (nk + nq), k = blockIdx.x % (nk + nq);
