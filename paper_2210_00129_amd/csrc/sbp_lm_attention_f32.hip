@@ -243,24 +243,16 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
     own_l = w.l2[((long long)b * a.h + h0) * w.npad + own];
     own_nd = w.nd[((long long)b * a.h + h0) * w.npad + own];
   }
-  // k, v (KEY) or q, dA of the own tokens: in registers, or, where these are short (d = 128 with them: 105 registers in memory, 734 us
-  // for 13 x 2 heads, 1273 tokens in documents of 300; without 523), in LDS
-  constexpr bool OWN = D < 128;
-  float f1[OWN ? D / 2 : 1], f2[OWN ? D / 2 : 1];
+  // k, v (KEY) or q, dA of the own tokens, in LDS: in registers they leave room for one wavefront per SIMD up to d = 64, and too little
+  // for d = 128 (13 x 2 heads, 1273 tokens in documents of 300: d = 64 283 us, 209 so; d = 128 613 us, 466 so)
   const float* p1 = qkv + own * ld + (KEY ? a.h + kv : h0) * D;
   const float* p2 = KEY ? p1 + a.hk * D : dA + own * lda + h0 * D;
-  if constexpr (OWN) {
-    F::row(p1, u, f1);
-    F::row(p2, u, f2);
-  } else {
-#pragma unroll
-    for (int c = D / 32 * wave; c < D / 32 * (wave + 1); ++c) {      // 8 dimensions each, a quarter per wavefront
-      float* at = img + (lane & 31) * F::PITCH + 8 * c + 4 * u;
-      *reinterpret_cast<float4*>(at) = *reinterpret_cast<const float4*>(p1 + 8 * c + 4 * u);
-      *reinterpret_cast<float4*>(at + 32 * F::PITCH) = *reinterpret_cast<const float4*>(p2 + 8 * c + 4 * u);
-    }
-    __syncthreads();
+  for (int c = wave; c < D / 8; c += 4) {                    // 8 dimensions each
+    float* at = img + (lane & 31) * F::PITCH + 8 * c + 4 * u;
+    *reinterpret_cast<float4*>(at) = *reinterpret_cast<const float4*>(p1 + 8 * c + 4 * u);
+    *reinterpret_cast<float4*>(at + 32 * F::PITCH) = *reinterpret_cast<const float4*>(p2 + 8 * c + 4 * u);
   }
+  __syncthreads();
   f32x16_t acc[KEY ? 2 : 1][F::DB];
 #pragma unroll
   for (int q = 0; q < (KEY ? 2 : 1); ++q)
@@ -299,14 +291,7 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
       tp[q4] = *reinterpret_cast<const f32x4_t*>(w.pos + at);
       td[q4] = *reinterpret_cast<const int4*>(w.doc + at);
     }
-    f32x16_t s, dp;
-    if constexpr (OWN) {
-      s = F::scores(x1, f1);
-      dp = F::scores(x2, f2);
-    } else {
-      s = F::scores(x1, img, lane);
-      dp = F::scores(x2, img + 32 * F::PITCH, lane);
-    }
+    f32x16_t s = F::scores(x1, img, lane), dp = F::scores(x2, img + 32 * F::PITCH, lane);
     float c[16][F::DB];                                      // (under way while the weights are worked out)
     F::columns(c, s1 + t0 * ld, ld, last, lane);
     __builtin_amdgcn_sched_barrier(0);
@@ -382,7 +367,7 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
 }
 
 template <int D, bool CAP>
-__global__ void __launch_bounds__(256, D <= 32 ? 2 : 1) masked_backward_f32_kernel(MaskedAttention a, LmTables w) {
+__global__ void __launch_bounds__(256, D <= 64 ? 2 : 1) masked_backward_f32_kernel(MaskedAttention a, LmTables w) {
   __shared__ __attribute__((aligned(16))) float img[4 * 32 * LmF32<D>::PITCH];
   __shared__ uint32_t again_s;
   const int nk = a.B * a.hk * w.parts, nq = a.B * a.h, blocks = (a.rows + 31) / 32, rank = blockIdx.x / (nk + nq), k = blockIdx.x % (nk + nq);
