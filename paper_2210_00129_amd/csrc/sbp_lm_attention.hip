@@ -1,11 +1,15 @@
 // Masked attention (sbp_lm.h): forward over all tokens of a sample and backward on the kept ones.
 #include <algorithm>
+#include <type_traits>
 
 #include "sbp_lm_attention_tiles.h"
 
 namespace sbp {
 
-template <typename T>
+// What the backward's main kernel reads per token (LmTables).  Bound: the read of A and dA (4 x 12 heads of 64, 1024 kept tokens: 12.6 MB, 5.3 us of
+// which most is the launch and one round trip to memory; 16 heads of 128, 4096 tokens: 33.5 MB, 7.3 us);
+// all of a wavefront's loads are under way at once.
+template <typename T, int D>
 __global__ void __launch_bounds__(256) masked_prepare_kernel(MaskedAttention a, LmTables w) {
   // a workgroup per tile and head (head h: positions and documents)
   const int tiles = w.npad / kLmTile, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -29,19 +33,26 @@ __global__ void __launch_bounds__(256) masked_prepare_kernel(MaskedAttention a, 
     if (lane == 0) w.range[(long long)b * tiles + tile] = make_int4(p0, p1, r.lo, r.hi);
     return;
   }
-  // delta of a row: d / 8 (bf16) or d / 4 (fp32) lanes of 16 bytes each
-  constexpr int N = 16 / sizeof(T);
-  const int per = a.d / N, rows = 64 / per;
-  const long long ld = (long long)a.h * a.d, row0 = (long long)b * a.rows, at = ((long long)b * a.h + head) * w.npad + tile * kLmTile;
-  for (int r0 = 16 * wave; r0 < 16 * wave + 16; r0 += rows) {
-    const int row = r0 + lane / per, tok = tile * kLmTile + row, c = lane % per * N;
-    float s = 0.f;
-    if (row < 16 * wave + 16 && tok < a.rows) s = lm_dot((const T*)a.dA + (row0 + tok) * ld + head * a.d + c, (const T*)a.A + (row0 + tok) * ld + head * a.d + c, N);
-    for (int m = 1; m < per; m <<= 1) s += __shfl_xor(s, m);
-    if (row < 16 * wave + 16 && lane % per == 0) w.nd[at + row] = -s;
+  // delta of a row: D / 8 (bf16) or D / 4 (fp32) lanes of 16 bytes each
+  constexpr int N = 16 / sizeof(T), PER = D / N, ROWS = 64 / PER < 16 ? 64 / PER : 16, IT = 16 / ROWS;
+  const long long ld = (long long)a.h * D, row0 = (long long)b * a.rows, at = ((long long)b * a.h + head) * w.npad + tile * kLmTile;
+  const float l = wave == 0 && on ? a.lse[(row0 + t) * a.h + head] : -INFINITY;
+  uint4 x[IT], y[IT];
+#pragma unroll
+  for (int i = 0; i < IT; ++i) {
+    const long long off = (row0 + min(tile * kLmTile + 16 * wave + i * ROWS + min(lane / PER, ROWS - 1), a.rows - 1)) * ld + head * D + lane % PER * N;
+    x[i] = *reinterpret_cast<const uint4*>((const T*)a.dA + off);
+    y[i] = *reinterpret_cast<const uint4*>((const T*)a.A + off);
+  }
+#pragma unroll
+  for (int i = 0; i < IT; ++i) {
+    const int row = 16 * wave + i * ROWS + lane / PER;
+    float s = tile * kLmTile + row < a.rows ? lm_dot((const T*)&x[i], (const T*)&y[i], N) : 0.f;
+#pragma unroll
+    for (int m = 1; m < PER; m <<= 1) s += __shfl_xor(s, m);
+    if (lane / PER < ROWS && lane % PER == 0) w.nd[at + row] = -s;
   }
   if (wave) return;
-  const float l = on ? a.lse[(row0 + t) * a.h + head] : -INFINITY;
   w.l2[at + lane] = l == -INFINITY ? 1e30f : l * (sizeof(T) == 2 ? kLog2e : 1.f);      // (a weight of exp(score - 1e30) = 0)
 }
 
@@ -62,11 +73,12 @@ __global__ void __launch_bounds__(256) masked_join_kernel(MaskedAttention a, LmT
   else *reinterpret_cast<float4*>(out) = s;
 }
 
-// Parts of a key / value head: its query heads follow one another in one workgroup per 128 keys (fp32: 32) unless that leaves fewer than
-// two workgroups per CU (256 CUs); then they are dealt to the smallest number of parts that does, each one more set of fp32 dK and dV.
+// Parts of a key / value head: its query heads follow one another in one workgroup per 128 keys (fp32: 32) unless that leaves fewer
+// workgroups of this kind than CUs (256); then they are dealt to the smallest number of parts that does not, each one more set of fp32
+// dK and dV.  (16 heads of 128 sharing 2, 4096 kept tokens: 4 parts 394 us, 2 parts 567, 8 parts 394 with twice the workspace.)
 static int masked_parts(int64_t heads, int share, int nchunks) {
   int p = 1;
-  while (p < share && heads * p * nchunks < 512) {
+  while (p < share && heads * p * nchunks < 256) {
     ++p;
     while (share % p) ++p;
   }
@@ -106,8 +118,15 @@ int32_t launch_backward_attention_masked(const MaskedAttention& a, const MaskedA
   const LmTables w{(float*)(ws + p.off_l2), (float*)(ws + p.off_nd), (float*)(ws + p.off_pos), (int32_t*)(ws + p.off_doc), (int4*)(ws + p.off_range),
                    p.parts > 1 ? (float*)(ws + p.off_part) : nullptr, p.npad, p.parts, p.nchunks};
   const dim3 prepare((unsigned)((int64_t)a.B * (a.h + 1) * (p.npad / kLmTile)));
-  if (bf16) SBP_LAUNCH(SBP_PROF_OTHER, s, (masked_prepare_kernel<uint16_t>), prepare, dim3(256), 0, s, a, w);
-  else SBP_LAUNCH(SBP_PROF_OTHER, s, (masked_prepare_kernel<float>), prepare, dim3(256), 0, s, a, w);
+  auto go = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    if (bf16) SBP_LAUNCH(SBP_PROF_OTHER, s, (masked_prepare_kernel<uint16_t, D>), prepare, dim3(256), 0, s, a, w);
+    else SBP_LAUNCH(SBP_PROF_OTHER, s, (masked_prepare_kernel<float, D>), prepare, dim3(256), 0, s, a, w);
+  };
+  if (a.d == 16) go(std::integral_constant<int, 16>{});
+  else if (a.d == 32) go(std::integral_constant<int, 32>{});
+  else if (a.d == 64) go(std::integral_constant<int, 64>{});
+  else go(std::integral_constant<int, 128>{});
   if (!bf16) launch_masked_f32(a, &w, s);
   else if (a.d == 16) launch_masked_backward_bf16<16>(a, w, s);
   else if (a.d == 32) launch_masked_backward_bf16<32>(a, w, s);
