@@ -178,7 +178,7 @@ int32_t sbp_forward_embedding(const void* tokens, int32_t token_bytes, const voi
 
 size_t sbp_backward_embedding_workspace(int64_t M, int64_t K, int64_t V, int32_t C, int32_t dtype, uint32_t flags) {
   if (validate_embedding_backward(M, K, V, C, 4, dtype, flags) != SBP_OK) return 0;
-  return plan_embedding_backward(K, V, C, dtype).bytes;
+  return plan_embedding_backward(K, V, C, flags).bytes;
 }
 
 int32_t sbp_backward_embedding(const void* dE, const void* tokens, int32_t token_bytes, const int32_t* idx, int64_t M, int64_t K, int64_t V,
@@ -190,7 +190,7 @@ int32_t sbp_backward_embedding(const void* dE, const void* tokens, int32_t token
   if (K > 0 && (!dE || !tokens)) return fail(SBP_ERR_NULL, "dE or tokens is NULL");
   if (!idx && K > 0 && K != M) return fail(SBP_ERR_NULL, "idx is NULL but K=%lld is not M=%lld", (long long)K, (long long)M);
   if ((uintptr_t)tokens % token_bytes) return fail(SBP_ERR_SHAPE, "tokens must be aligned to their size");
-  const EmbeddingPlan p = plan_embedding_backward(K, V, C, dtype);
+  const EmbeddingPlan p = plan_embedding_backward(K, V, C, flags);
   st = check_workspace(ws, ws_bytes, p.bytes);
   if (st != SBP_OK) return st;
   return launch_backward_embedding(p, dE, tokens, token_bytes, idx, M, K, V, C, scale, dtype, dtable, ws, flags,

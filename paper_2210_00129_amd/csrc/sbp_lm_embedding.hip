@@ -36,7 +36,8 @@ __device__ __forceinline__ void em_put(uint16_t* p, float v) { *p = (uint16_t)bf
 template <typename K>
 __device__ __forceinline__ long long em_token(const K* tokens, const int32_t* idx, long long j) { return (long long)tokens[idx ? idx[j] : j]; }
 
-// ---- lookup: one piece of 16 bytes (VEC) or one channel per thread and step ----------------------------------------
+// ---- lookup: a wavefront per row, a piece of 16 bytes (VEC) or one channel per lane and step.  Bound: HBM (32768 rows of 2048 channels, bf16,
+// out of 50000: 256 MB in 48 us) ----------------------------------------
 template <typename T, typename K, bool VEC>
 __global__ void __launch_bounds__(256) embedding_forward_kernel(const K* __restrict__ tokens, const T* __restrict__ table, long long M, long long V,
                                                                 int C, float scale, T* __restrict__ E) {
@@ -66,15 +67,21 @@ __global__ void __launch_bounds__(256) embedding_forward_kernel(const K* __restr
 // of the whole table (dense, as the weight gradients of the other layers are); the grouping moves 8 bytes per kept row.
 //
 // Up to kEmScan kept rows one launch does it all: every wavefront owns some table rows and looks for each of them through the
-// kept tokens in LDS.  More rows are sorted by token (stable least-significant-digit radix sort of (token, row) pairs): up to
-// kEmOne of them by one workgroup with the pairs in registers and LDS, all passes in one launch; more by 64 workgroups, one launch
-// per pass.  The rest of that (first) launch zeroes the table, which takes longer than the sort of one workgroup for tables of
-// about 60 MB and more.  Then a wavefront sums chunks of kEmChunk sorted rows in order and writes the rows of the tokens that
-// end there, and tokens that cross a chunk's border are joined from partial sums in chunk order: every sum runs in the order of idx
-// whatever the grid does.
+// kept tokens in LDS.  (1000 rows of 200 channels, fp32, 198 kept: 9 us with the lookup's 2, sorted 17; but a token that all rows share is
+// then summed by one wavefront.)
+// More rows are sorted by token (stable least-significant-digit radix sort of (token, row) pairs): by one workgroup with the pairs in
+// registers and LDS, all passes in one launch, or by 64 workgroups, one launch per pass.  The rest of the (first) launch zeroes the table.
+// One workgroup: up to kEmOne rows, and up to kEmOneFill of them where zeroing kEmFill bytes or more hides a part of its time
+// (2048 channels, lookup and gradient; one workgroup and 64: 4000 rows, 500 / 16000 / 32000 tokens: 29 and 28, 40 and 55, 65 and 84 us; 8000
+// rows: 55 and 39, 71 and 74, 91 and 110; 16384 rows: 76 and 58, 122 and 119, 135 and 153).
+// Then a wavefront sums chunks of kEmChunk sorted rows in order and writes the rows of the tokens that end there, and tokens that cross
+// a chunk's border are joined from partial sums in chunk order: every sum runs in the order of idx whatever the grid does.
+// 50000 tokens of 2048 channels, 16384 kept rows, bf16, V C 4 = 410 MB: sort and zeroing 58 us (7 TB/s), sums 42, joins 6.
 // ------------------------------------------------------------------------------------------------
-// One launch costs less than the sort's three, but a token that all rows share is then summed by one wavefront.
-static constexpr int kEmScan = 256, kEmOne = 16384, kEmChunk = 32, kEmBins = 2048, kEmBlocks = 64;
+static constexpr int kEmScan = 256, kEmOne = 4096, kEmOneFill = 16384, kEmChunk = 32, kEmBins = 2048, kEmBlocks = 64;
+static constexpr int64_t kEmFill = 100 << 20;
+
+static int64_t em_fill_bytes(int64_t V, int32_t C, uint32_t flags) { return flags & SBP_FLAG_ACCUMULATE_DW ? 0 : V * C * (flags & SBP_FLAG_DW_OUT_BF16 ? 2 : 4); }
 
 // A lane's columns of one row: a piece of 16 bytes of the input (VEC) or one column.
 template <typename T, bool VEC>
@@ -470,13 +477,14 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const uint32_t* __r
   Cols::put(out + (long long)key * C + c0, s, scale, accumulate != 0);
 }
 
-EmbeddingPlan plan_embedding_backward(int64_t K, int64_t V, int32_t C, int32_t) {
+EmbeddingPlan plan_embedding_backward(int64_t K, int64_t V, int32_t C, uint32_t flags) {
   EmbeddingPlan p = {};
   p.sorted = K > kEmScan;
   if (!p.sorted) return p;
   int need = 1;                                             // bits of the keys 0 .. V
   while (V >> need) ++need;
-  if (K <= kEmOne) {
+  p.one = K <= kEmOne || (K <= kEmOneFill && em_fill_bytes(V, C, flags) >= kEmFill);
+  if (p.one) {
     p.nblocks = 1;
     p.passes = (int)ceil_div(need, 8);
   } else {
@@ -489,7 +497,7 @@ EmbeddingPlan plan_embedding_backward(int64_t K, int64_t V, int32_t C, int32_t) 
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
   for (int i = 0; i < 2; ++i) { p.off_keys[i] = take(4 * K); p.off_rows[i] = take(4 * K); }
-  p.off_hist = take(K <= kEmOne ? 0 : (size_t)p.passes * p.nblocks * (4 << p.bits));
+  p.off_hist = take(p.one ? 0 : (size_t)p.passes * p.nblocks * (4 << p.bits));
   p.off_partial = take((size_t)p.chunks * 2 * C * 4);
   p.bytes = at;
   return p;
@@ -536,10 +544,10 @@ static void launch_em_bwd(const EmbeddingPlan& p, const void* dE, const void* to
     return;
   }
   char* ws = (char*)ws_;
-  const long long fill = accumulate ? 0 : (long long)V * C * (long long)sizeof(O);
+  const long long fill = em_fill_bytes(V, C, flags);
   const uint32_t* keys;
   const int32_t* rows;
-  if (Kn <= kEmOne) {
+  if (p.one) {
     uint32_t* ko = (uint32_t*)(ws + p.off_keys[0]);
     int32_t* ro = (int32_t*)(ws + p.off_rows[0]);
     // (a filling workgroup has one piece of 16 bytes per thread at least, and the chip holds about two of these workgroups per CU)

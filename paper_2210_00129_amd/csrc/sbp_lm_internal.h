@@ -37,7 +37,7 @@ int32_t launch_backward_attention_masked(const MaskedAttention& a, const MaskedA
 // ---- norms between blocks ----------------------------------------------------------------------
 struct ResidualNormPlan {
   int    nblocks;                // workgroups per group of rows, and partial sums of each parameter gradient
-  size_t off_partial;            // fp32 [G][nblocks][4][C]
+  size_t off_partial;            // fp32 [G][nblocks][2 or 4][C]
   size_t off_inv;                // int32 [M]
   size_t bytes;
 };
@@ -51,13 +51,14 @@ int32_t launch_backward_residual_norm(const ResidualNormPlan& p, const sbp_resid
 // ---- token table -------------------------------------------------------------------------------
 struct EmbeddingPlan {
   bool    sorted;                // else every wavefront looks through the kept tokens for its own table rows
+  bool    one;                   // sort: one workgroup, in registers and LDS
   int     nblocks;               // sort: workgroups, each over a run of `per` kept rows
   int64_t per;
   int     passes, bits;          // sort: digits and bits of one
   int     chunks;                // runs of sorted rows that one wavefront sums
   size_t  off_keys[2], off_rows[2], off_hist, off_partial, bytes;
 };
-EmbeddingPlan plan_embedding_backward(int64_t K, int64_t V, int32_t C, int32_t dtype);
+EmbeddingPlan plan_embedding_backward(int64_t K, int64_t V, int32_t C, uint32_t flags);
 int32_t launch_forward_embedding(const void* tokens, int32_t token_bytes, const void* table, int64_t M, int64_t V, int32_t C, float scale,
                                  int32_t dtype, void* E, hipStream_t s);
 int32_t launch_backward_embedding(const EmbeddingPlan& p, const void* dE, const void* tokens, int32_t token_bytes, const int32_t* idx,

@@ -148,3 +148,11 @@ def test_the_binding_refuses_what_does_not_fit():
                       (lambda: sbp.backward_embedding(t[:4], tok, 6, dtable=t.bfloat16()), TypeError)]:
         with pytest.raises(err):
             call()
+
+
+@pytest.mark.parametrize("M,V,C,dtype,kind", [(5000, 60000, 512, "bf16", "zipf"), (16000, 70000, 384, "f32", "outside")])
+def test_gradient_of_a_table_that_takes_longer_to_clear_than_to_sort(M, V, C, dtype, kind):
+    rng = np.random.default_rng(3)
+    tok, dE = torch.from_numpy(_tokens(kind, M, V, rng)), torch.from_numpy(rng.standard_normal((M, C))).to(DT[dtype])
+    got = sbp.backward_embedding(dE.cuda(), tok.cuda(), V, scale=1.7)
+    _check_gradient(got, tok, dE, V, 1.7, "f32")
