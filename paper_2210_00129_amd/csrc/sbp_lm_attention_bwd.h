@@ -15,10 +15,11 @@
 // Tiles of which the workgroup sees nothing are left out of the list (ranges of positions and documents per tile; any order of the kept
 // tokens is right, ascending order makes it short).  Tiles that are visible altogether come first, in a loop without mask arithmetic.
 // Where a result is not finite, its row is computed again one row at a time (see sbp_lm_attention_fwd.h).
-// Bound, d = 128 (one wavefront per SIMD): the LDS, whose reads for a turn take as long as its products (a third of their cycles are
-// conflicts), and, capped, the vector arithmetic; 16 heads sharing 2, 4096 of 8192 tokens, causal, capped: 343 .. 394 us on the cards
-// seen with the first kernel's 7 and the last one's 5, uncapped 307.  d = 64: vector arithmetic and the chain of a workgroup's tiles;
-// 4 x 12 heads of 64, 1024 of 2048 tokens in documents of 300, biased: 37 .. 41 us; 16 samples of it 124.
+// Bound, d = 128 (one wavefront per SIMD): what one wavefront can issue; counted over the busy cycles of a CU, capped, the matrix cores are busy
+// 35 %, the vector units 49 %, the LDS 31 % (a layout without its conflicts: no gain), uncapped 44, 33 and 38 %, at a clock of 2.1 GHz.
+// 16 heads sharing 2, 4096 of 8192 tokens, causal, capped: 343 .. 380 us on the cards seen with the first kernel's 7 and the last one's 5,
+// uncapped 296.  d = 64: vector arithmetic and the chain of a workgroup's tiles; 4 x 12 heads of 64, 1024 of 2048 tokens in documents of
+// 300, biased: 37 .. 41 us (a CU is busy 63 % of it on average); 16 samples of it 121.
 #ifndef SBP_LM_ATTENTION_BWD_H_
 #define SBP_LM_ATTENTION_BWD_H_
 
@@ -381,17 +382,20 @@ template <int D, int MODE>
 __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) masked_backward_kernel(MaskedAttention a, LmTables w) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int list_s[kLmBwdList], count_s[2];
-  // units of one rank: the key groups and the query heads of all samples; the heads of one XCD stay on it where both divide by 8
-  const int nk = a.B * a.hk * w.parts, nq = a.B * a.h, i = blockIdx.x;
+  // Units: the key groups and the query heads of all samples, each for every rank; those of one XCD stay on it where both divide by 8.
+  // d = 128 (one workgroup on a CU): all key units first, the longer kind (the long text 379 us, mixed by rank 391).  Smaller heads (two): mixed,
+  // since a key and a query unit share a CU better than two key units (packed documents 41 us, key units first 44).
+  const int nk = a.B * a.hk * w.parts, nq = a.B * a.h, x8 = nk % 8 == 0 && nq % 8 == 0 ? 8 : 1, pk = nk / x8, pq = nq / x8;
+  const int x = blockIdx.x % x8, j = blockIdx.x / x8;
   int rank, k;
-  if (nk % 8 == 0 && nq % 8 == 0) {
-    const int pk = nk / 8, pq = nq / 8, j = i >> 3, x = i & 7;
+  if (D == 128) {
+    const int q = j - pk * w.nchunks;
+    rank = q < 0 ? j / pk : q / pq;
+    k = q < 0 ? x * pk + j % pk : nk + x * pq + q % pq;
+  } else {
     rank = j / (pk + pq);
     k = j % (pk + pq);
     k = k < pk ? x * pk + k : nk + x * pq + k - pk;
-  } else {
-    rank = i / (nk + nq);
-    k = i % (nk + nq);
   }
   // causal: the first keys are seen by the most queries, the last queries see the most keys
   if (k < nk) masked_backward_body<D, true, MODE>(smem, list_s, count_s, a, w, k / (a.hk * w.parts), k % (a.hk * w.parts), rank);
