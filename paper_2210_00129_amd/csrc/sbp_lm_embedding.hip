@@ -40,15 +40,15 @@ __device__ __forceinline__ long long em_token(const K* tokens, const int32_t* id
 // out of 50000: 256 MB in 48 us) ----------------------------------------
 template <typename T, typename K, bool VEC>
 __global__ void __launch_bounds__(256) embedding_forward_kernel(const K* __restrict__ tokens, const T* __restrict__ table, long long M, long long V,
-                                                                int C, float scale, T* __restrict__ E) {
+                                                                int C, int slice, float scale, T* __restrict__ E) {
   constexpr int N = VEC ? EmPiece<T>::N : 1;
-  const int per_row = C / N, lane = threadIdx.x & 63;
-  // a wavefront takes a row
+  const int lane = threadIdx.x & 63, first = blockIdx.y * slice, per_row = min(first + slice, C / N);
+  // a wavefront takes a slice of a row
   for (long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); r < M; r += (long long)gridDim.x * 4) {
     const long long tok = (long long)tokens[r];
     const bool ok = tok >= 0 && tok < V;
     const T* src = table + (ok ? tok : 0) * C;
-    for (int p = lane; p < per_row; p += 64) {
+    for (int p = first + lane; p < per_row; p += 64) {
       if constexpr (VEC) {
         float v[N];
         EmPiece<T>::load(src + p * N, v);
@@ -66,9 +66,8 @@ __global__ void __launch_bounds__(256) embedding_forward_kernel(const K* __restr
 // Gradient.  dtable[v] = scale * sum of the kept rows of dE whose token is v.  The floor is the read of the kept rows and the write
 // of the whole table (dense, as the weight gradients of the other layers are); the grouping moves 8 bytes per kept row.
 //
-// Up to kEmScan kept rows one launch does it all: every wavefront owns some table rows and looks for each of them through the
-// kept tokens in LDS.  (1000 rows of 200 channels, fp32, 198 kept: 9 us with the lookup's 2, sorted 17; but a token that all rows share is
-// then summed by one wavefront.)
+// Up to kEmScan kept rows one launch does it all: every workgroup owns some table rows and looks through the kept tokens for them.
+// (1000 rows of 200 channels, fp32, 198 kept: 10 us with the lookup's 2, sorted 17.)
 // More rows are sorted by token (stable least-significant-digit radix sort of (token, row) pairs): by one workgroup with the pairs in
 // registers and LDS, all passes in one launch, or by 64 workgroups, one launch per pass.  The rest of the (first) launch zeroes the table.
 // One workgroup: up to kEmOne rows, and up to kEmOneFill of them where zeroing kEmFill bytes or more hides a part of its time
@@ -119,64 +118,92 @@ struct EmCols {
   }
 };
 
+// Zeroes the bytes from `begin` to `end` (multiples of sizeof(O)), thread `t` of `threads`: whole pieces of 16 bytes by their addresses, and
+// what lies before and behind them.
+template <typename O>
+__device__ __forceinline__ void em_zero(char* begin, char* end, long long t, long long threads) {
+  char *head = (char*)(((uintptr_t)begin + 15) & ~(uintptr_t)15), *tail = (char*)((uintptr_t)end & ~(uintptr_t)15);
+  if (head > end) head = end;
+  if (tail < head) tail = head;
+  for (long long i = t; i < (tail - head) / 16; i += threads) reinterpret_cast<uint4*>(head)[i] = make_uint4(0, 0, 0, 0);
+  if (t < 16 / (long long)sizeof(O)) {
+    if (begin + t * sizeof(O) < head) reinterpret_cast<O*>(begin)[t] = 0;
+    if (tail + t * sizeof(O) < end) reinterpret_cast<O*>(tail)[t] = 0;
+  }
+}
+
+// A workgroup owns `rows` table rows and, of these, a slice of the columns (all of them where there are rows enough for every CU).  It zeroes
+// its part, and sums the rows of the tokens that it finds among the kept ones, in their order.
 template <typename T, typename K, typename O, bool VEC>
 __global__ void __launch_bounds__(256) embedding_scan_kernel(const T* __restrict__ dE, const K* __restrict__ tokens, const int32_t* __restrict__ idx,
-                                                             int Kn, long long V, int C, int rows_per_wave, float scale, int compact, int accumulate,
+                                                             int Kn, long long V, int C, int rows, int slice, float scale, int compact, int accumulate,
                                                              O* __restrict__ out) {
   using Cols = EmCols<T, VEC>;
-  constexpr int N = Cols::N, U = 4;
-  __shared__ int tok_s[kEmScan], row_s[kEmScan];
+  constexpr int N = Cols::N, U = 8, Q = kEmScan / 64;
+  __shared__ int tok_s[kEmScan], row_s[kEmScan], list_s[4][kEmScan];
   const int t = threadIdx.x, lane = t & 63;
+  int* list = list_s[t >> 6];
+  const int first = blockIdx.y * slice, last = min(first + slice, C);
+  const long long v0 = (long long)blockIdx.x * rows, v1 = min(v0 + rows, V);
   if (t < Kn) {
     const long long tok = em_token(tokens, idx, t);
-    tok_s[t] = tok >= 0 && tok < V ? (int)tok : -1;
+    tok_s[t] = tok >= v0 && tok < v1 ? (int)(tok - v0) : -1;
     row_s[t] = compact || !idx ? t : idx[t];
   } else {
     tok_s[t] = -1;
   }
   __syncthreads();
-  const long long v0 = ((long long)blockIdx.x * 4 + (t >> 6)) * rows_per_wave, v1 = min(v0 + rows_per_wave, V);
-  int tk[kEmScan / 64];
+  int tk[Q];
+  unsigned long long left[Q], any = 0;                     // the same for all wavefronts
 #pragma unroll
-  for (int q = 0; q < kEmScan / 64; ++q) tk[q] = tok_s[64 * q + lane];
-  for (long long v = v0; v < v1; ++v) {
-    unsigned long long hit[kEmScan / 64], any = 0;
-#pragma unroll
-    for (int q = 0; q < kEmScan / 64; ++q) { hit[q] = __ballot(tk[q] == (int)v); any |= hit[q]; }
-    if (accumulate && !any) continue;
-    for (int c0 = lane * N; c0 < C; c0 += Cols::SLICE) {
-      float s[N];
-#pragma unroll
-      for (int e = 0; e < N; ++e) s[e] = 0.f;
-      for (int q = 0; any && q < kEmScan / 64; ++q) {
-        unsigned long long w = hit[q];
-        while (w) {                                        // U rows in flight, added in order
-          typename Cols::Raw x[U];
-          int n = 0;
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            if (!w) break;
-            x[u] = Cols::load(dE + (long long)row_s[64 * q + __ffsll((long long)w) - 1] * C + c0);
-            w &= w - 1;
-            n = u + 1;
-          }
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            if (u < n) Cols::add(x[u], s);
-        }
-      }
-      Cols::put(out + v * C + c0, s, scale, accumulate != 0);
+  for (int q = 0; q < Q; ++q) {
+    tk[q] = tok_s[64 * q + lane];
+    left[q] = __ballot(tk[q] >= 0);
+    any |= left[q];
+  }
+  if (!accumulate && !(rows == 1 && any)) {                  // (a row alone whose token occurs is written below)
+    if (slice >= C) em_zero<O>((char*)(out + v0 * C), (char*)(out + v1 * C), t, 256);
+    else
+      for (long long v = v0; v < v1; ++v) em_zero<O>((char*)(out + v * C + first), (char*)(out + v * C + last), t, 256);
+    if (any) {                                               // other threads write some of these places again
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
     }
   }
-}
-
-// Zeroes a run of 16-byte pieces (and the bytes behind them), all threads of `blocks` workgroups of NT together.
-template <int NT>
-__device__ __forceinline__ void em_fill(char* out, long long bytes, int block, int blocks) {
-  const long long pieces = bytes / 16, step = (long long)blocks * NT;
-  for (long long i = (long long)block * NT + threadIdx.x; i < pieces; i += step) reinterpret_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
-  if (block == 0)
-    for (long long i = pieces * 16 + 2 * (long long)threadIdx.x; i < bytes; i += 2 * NT) *reinterpret_cast<uint16_t*>(out + i) = 0;
+#pragma unroll
+  for (int q0 = 0; q0 < Q; ++q0)
+    while (left[q0]) {
+      const int v = __builtin_amdgcn_readlane(tk[q0], __ffsll((long long)left[q0]) - 1);
+      unsigned long long hit[Q];
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        hit[q] = __ballot(tk[q] == v);
+        left[q] &= ~hit[q];
+      }
+      // the token's rows in order: a list of the wavefront's own (its LDS accesses complete in order)
+      int count = 0;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        if (tk[q] == v) list[count + __popcll(hit[q] & ((1ull << lane) - 1))] = row_s[64 * q + lane];
+        count += __popcll(hit[q]);
+      }
+      __builtin_amdgcn_wave_barrier();
+      for (int c0 = first + t * N; c0 < last; c0 += 256 * N) {
+        float s[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[e] = 0.f;
+        for (int i = 0; i < count; i += U) {                 // U rows in flight (past the end the last one again, unused), added in order
+          typename Cols::Raw x[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) x[u] = Cols::load(dE + (long long)list[min(i + u, count - 1)] * C + c0);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (i + u < count) Cols::add(x[u], s);
+        }
+        Cols::put(out + (v0 + v) * C + c0, s, scale, accumulate != 0);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // ---- sort ----------------------------------------------------------------------------------------------------------
@@ -193,12 +220,12 @@ __device__ __forceinline__ unsigned long long em_same(uint32_t digit, bool on, i
 // One workgroup of 16 wavefronts, all passes: every wavefront holds a run of the elements in registers (R rounds of 64), finds an
 // element's place among the wavefront's own, and after the counts of all wavefronts have been added up writes it to its place in LDS.
 // The other workgroups of the launch zero the table.
-template <typename K, int R>
+template <typename K, typename O, int R>
 __global__ void __launch_bounds__(1024) embedding_sort_kernel(const K* __restrict__ tokens, const int32_t* __restrict__ idx, int compact, int Kn,
                                                               long long V, int bits, int passes, uint32_t* __restrict__ keys_out,
                                                               int32_t* __restrict__ rows_out, char* __restrict__ table, long long table_bytes) {
   if (blockIdx.x) {
-    em_fill<1024>(table, table_bytes, blockIdx.x - 1, gridDim.x - 1);
+    em_zero<O>(table, table + table_bytes, (blockIdx.x - 1) * 1024LL + threadIdx.x, (gridDim.x - 1) * 1024LL);
     return;
   }
   extern __shared__ uint32_t em_lds[];
@@ -278,13 +305,13 @@ __global__ void __launch_bounds__(1024) embedding_sort_kernel(const K* __restric
 
 // 64 workgroups: kept row j belongs to block b = j / per.  hist[p][b][digit]: how many elements of block b (in the order before pass p)
 // have the digit.  The workgroups behind the first nb zero the table.
-template <typename K>
+template <typename K, typename O>
 __global__ void __launch_bounds__(256) embedding_count_kernel(const K* __restrict__ tokens, const int32_t* __restrict__ idx, int Kn, long long V,
                                                               int per, int nb, int bits, int passes, uint32_t* __restrict__ hist,
                                                               char* __restrict__ table, long long table_bytes) {
   __shared__ uint32_t bins_s[kEmBins];
   if ((int)blockIdx.x >= nb) {
-    em_fill<256>(table, table_bytes, blockIdx.x - nb, gridDim.x - nb);
+    em_zero<O>(table, table + table_bytes, (blockIdx.x - nb) * 256LL + threadIdx.x, (gridDim.x - nb) * 256LL);
     return;
   }
   const int t = threadIdx.x, bins = 1 << bits;
@@ -506,9 +533,12 @@ EmbeddingPlan plan_embedding_backward(int64_t K, int64_t V, int32_t C, uint32_t 
 template <typename T, typename K>
 static void launch_em_fwd(const void* tokens, const void* table, int64_t M, int64_t V, int32_t C, float scale, void* E, hipStream_t s) {
   const bool vec = C % EmPiece<T>::N == 0 && ((uintptr_t)table | (uintptr_t)E) % 16 == 0;
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(M, 4), 1 << 20));
-  if (vec) SBP_LAUNCH(SBP_PROF_GATHER, s, (embedding_forward_kernel<T, K, true>), grid, dim3(256), 0, s, (const K*)tokens, (const T*)table, (long long)M, (long long)V, C, scale, (T*)E);
-  else SBP_LAUNCH(SBP_PROF_GATHER, s, (embedding_forward_kernel<T, K, false>), grid, dim3(256), 0, s, (const K*)tokens, (const T*)table, (long long)M, (long long)V, C, scale, (T*)E);
+  // a wavefront per row; fewer than 2048 rows are cut into slices of 64 pieces or more (3 rows of 3493 channels: one wavefront each takes 55 turns)
+  const int64_t pieces = vec ? C / EmPiece<T>::N : C, cuts = std::max<int64_t>(1, std::min<int64_t>(ceil_div(pieces, 64), 2048 / std::max<int64_t>(M, 1)));
+  const int slice = (int)align_up((size_t)ceil_div(pieces, cuts), 64);
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(M, 4), 1 << 20), (unsigned)ceil_div(pieces, slice));
+  if (vec) SBP_LAUNCH(SBP_PROF_GATHER, s, (embedding_forward_kernel<T, K, true>), grid, dim3(256), 0, s, (const K*)tokens, (const T*)table, (long long)M, (long long)V, C, slice, scale, (T*)E);
+  else SBP_LAUNCH(SBP_PROF_GATHER, s, (embedding_forward_kernel<T, K, false>), grid, dim3(256), 0, s, (const K*)tokens, (const T*)table, (long long)M, (long long)V, C, slice, scale, (T*)E);
 }
 
 int32_t launch_forward_embedding(const void* tokens, int32_t token_bytes, const void* table, int64_t M, int64_t V, int32_t C, float scale,
@@ -537,10 +567,13 @@ static void launch_em_bwd(const EmbeddingPlan& p, const void* dE, const void* to
   const bool vec = C % EmPiece<T>::N == 0 && ((uintptr_t)dE | (uintptr_t)out) % 16 == 0;
   const int compact = flags & SBP_FLAG_DY_COMPACT ? 1 : 0, accumulate = flags & SBP_FLAG_ACCUMULATE_DW ? 1 : 0;
   if (!p.sorted) {
-    const int rpw = (int)std::max<int64_t>(1, ceil_div(V, 4 * 2048));      // table rows per wavefront: at most 2048 workgroups read the tokens
-    const dim3 grid((unsigned)ceil_div(V, 4 * rpw));
-    if (vec) SBP_LAUNCH(SBP_PROF_REDUCE, s, (embedding_scan_kernel<T, K, O, true>), grid, dim3(256), 0, s, (const T*)dE, (const K*)tokens, idx, (int)Kn, (long long)V, C, rpw, scale, compact, accumulate, (O*)out);
-    else SBP_LAUNCH(SBP_PROF_REDUCE, s, (embedding_scan_kernel<T, K, O, false>), grid, dim3(256), 0, s, (const T*)dE, (const K*)tokens, idx, (int)Kn, (long long)V, C, rpw, scale, compact, accumulate, (O*)out);
+    // table rows per workgroup: at most 2048 workgroups read the tokens; fewer than 1024 rows are cut into slices of 256 pieces or more
+    const int rows = (int)std::max<int64_t>(1, ceil_div(V, 2048));
+    const int64_t n = vec ? EmPiece<T>::N : 1, cuts = std::max<int64_t>(1, std::min<int64_t>(ceil_div(C, 256 * n), 1024 / V));
+    const int slice = (int)std::min<int64_t>(C, align_up((size_t)ceil_div(C, cuts), 256 * (size_t)n));
+    const dim3 grid((unsigned)ceil_div(V, rows), (unsigned)ceil_div(C, slice));
+    if (vec) SBP_LAUNCH(SBP_PROF_REDUCE, s, (embedding_scan_kernel<T, K, O, true>), grid, dim3(256), 0, s, (const T*)dE, (const K*)tokens, idx, (int)Kn, (long long)V, C, rows, slice, scale, compact, accumulate, (O*)out);
+    else SBP_LAUNCH(SBP_PROF_REDUCE, s, (embedding_scan_kernel<T, K, O, false>), grid, dim3(256), 0, s, (const T*)dE, (const K*)tokens, idx, (int)Kn, (long long)V, C, rows, slice, scale, compact, accumulate, (O*)out);
     return;
   }
   char* ws = (char*)ws_;
@@ -555,8 +588,8 @@ static void launch_em_bwd(const EmbeddingPlan& p, const void* dE, const void* to
     auto go = [&](auto r) {
       constexpr int R = decltype(r)::value;
       const size_t lds = (size_t)(2 * R * 1024 + 16 * 256) * 4;
-      allow_dynamic_lds(reinterpret_cast<const void*>(embedding_sort_kernel<K, R>), lds);
-      SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_sort_kernel<K, R>), dim3(1 + fillers), dim3(1024), lds, s, (const K*)tokens, idx, compact, (int)Kn, (long long)V,
+      allow_dynamic_lds(reinterpret_cast<const void*>(embedding_sort_kernel<K, O, R>), lds);
+      SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_sort_kernel<K, O, R>), dim3(1 + fillers), dim3(1024), lds, s, (const K*)tokens, idx, compact, (int)Kn, (long long)V,
                  p.bits, p.passes, ko, ro, (char*)out, fill);
     };
     if (Kn <= 1024) go(std::integral_constant<int, 1>{});
@@ -566,7 +599,7 @@ static void launch_em_bwd(const EmbeddingPlan& p, const void* dE, const void* to
   } else {
     uint32_t* hist = (uint32_t*)(ws + p.off_hist);
     const unsigned fillers = (unsigned)std::min<long long>(ceil_div(fill, 16 * 256), 2048);
-    SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_count_kernel<K>), dim3(p.nblocks + fillers), dim3(256), 0, s, (const K*)tokens, idx, (int)Kn, (long long)V, (int)p.per,
+    SBP_LAUNCH(SBP_PROF_OTHER, s, (embedding_count_kernel<K, O>), dim3(p.nblocks + fillers), dim3(256), 0, s, (const K*)tokens, idx, (int)Kn, (long long)V, (int)p.per,
                p.nblocks, p.bits, p.passes, hist, (char*)out, fill);
     for (int q = 0; q < p.passes; ++q) {
       uint32_t *ki = (uint32_t*)(ws + p.off_keys[(q + 1) & 1]), *ko = (uint32_t*)(ws + p.off_keys[q & 1]);

@@ -156,3 +156,26 @@ def test_gradient_of_a_table_that_takes_longer_to_clear_than_to_sort(M, V, C, dt
     tok, dE = torch.from_numpy(_tokens(kind, M, V, rng)), torch.from_numpy(rng.standard_normal((M, C))).to(DT[dtype])
     got = sbp.backward_embedding(dE.cuda(), tok.cuda(), V, scale=1.7)
     _check_gradient(got, tok, dE, V, 1.7, "f32")
+
+
+@pytest.mark.parametrize("M,V,C,dtype,kind", [(3, 67, 3493, "bf16", "even"), (120, 30, 1031, "bf16", "zipf"), (250, 7, 2050, "f32", "one"), (15, 15000, 346, "f32", "outside"),
+                                              (200, 5000, 61, "bf16", "zipf")])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_few_rows_of_many_channels(M, V, C, dtype, kind, shift):
+    """Rows cut into slices of columns; outputs that start between two pieces of 16 bytes, whose neighbours stay as they are."""
+    tok, table, dE, _ = _case(M, V, C, dtype, kind, seed=5)
+    ref = lm.embedding(tok.numpy(), f64(table), float(np.float32(0.7)))
+    E = torch.full((M * C + 16,), 7.0, dtype=DT[dtype], device="cuda")
+    sbp.forward_embedding(tok.cuda(), table.cuda(), 0.7, out=E[shift:shift + M * C].view(M, C))
+    within(E[shift:shift + M * C].view(M, C), ref, np.abs(ref) * (out_step(dtype) + 2.0 ** -24), "E")
+    assert (E[:shift] == 7).all() and (E[shift + M * C:] == 7).all()
+    for flags, out in ((0, "f32"), (sbp.FLAG_DW_OUT_BF16, "bf16")):
+        got = torch.full((V * C + 16,), 7.0, dtype=DT[out], device="cuda")
+        part = got[shift:shift + V * C].view(V, C)
+        sbp.backward_embedding(dE.cuda(), tok.cuda(), V, scale=0.7, flags=flags, dtable=part)
+        _check_gradient(part, tok, dE, V, 0.7, out)
+        assert (got[:shift] == 7).all() and (got[shift + V * C:] == 7).all()
+    base = torch.randn(V, C, device="cuda")
+    got = torch.empty(V * C + 1, device="cuda")[shift:shift + V * C].view(V, C).copy_(base)
+    sbp.backward_embedding(dE.cuda(), tok.cuda(), V, scale=0.7, flags=sbp.FLAG_ACCUMULATE_DW, dtable=got)
+    _check_gradient(got, tok, dE, V, 0.7, "f32", base=base)
