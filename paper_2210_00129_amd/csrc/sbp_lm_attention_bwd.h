@@ -17,9 +17,9 @@
 // Where a result is not finite, its row is computed again one row at a time (see sbp_lm_attention_fwd.h).
 // Bound, d = 128 (one wavefront per SIMD): what one wavefront can issue; counted over the busy cycles of a CU, capped, the matrix cores are busy
 // 35 %, the vector units 49 %, the LDS 31 % (a layout without its conflicts: no gain), uncapped 44, 33 and 38 %, at a clock of 2.1 GHz.
-// 16 heads sharing 2, 4096 of 8192 tokens, causal, capped: 343 .. 380 us on the cards seen with the first kernel's 7 and the last one's 5,
+// 16 heads sharing 2, 4096 of 8192 tokens, causal, capped: 330 .. 380 us on the cards seen with the first kernel's 7 and the last one's 5,
 // uncapped 296.  d = 64: vector arithmetic and the chain of a workgroup's tiles; 4 x 12 heads of 64, 1024 of 2048 tokens in documents of
-// 300, biased: 37 .. 41 us (a CU is busy 63 % of it on average); 16 samples of it 121.
+// 500 on average, biased: 35 .. 41 us (a CU is busy 63 % of it on average); 16 samples of it 121.
 #ifndef SBP_LM_ATTENTION_BWD_H_
 #define SBP_LM_ATTENTION_BWD_H_
 

@@ -20,10 +20,10 @@
 // finite, its row is computed again one row at a time, without the keys it does not see.
 // Bound, d = 128: the products of one half against the vector arithmetic of the other, at the clock that the card keeps under them (counted over the
 // busy cycles of a CU, capped: matrix cores 41 %, vector units 64 %, LDS 31 %, 1.95 GHz; uncapped 51, 46, 40 %, 1.9 GHz); 16 heads sharing
-// 2, 8192 tokens, causal, capped: 313 .. 355 us on the cards seen (275 GFLOP counted, 0.8 .. 0.9 PFLOP/s), uncapped 280 (0.98).
+// 2, 8192 tokens, causal, capped: 302 .. 355 us on the cards seen (275 GFLOP counted, 0.8 .. 0.9 PFLOP/s), uncapped 280 (0.98).
 // d = 64: vector arithmetic, and for short documents the chain of a workgroup's few tiles (1.25 us each with one workgroup on a CU, some 8 us
 // before and after them) and their unequal number (a CU is busy half of the time on average); 4 x 12 heads of 64, 2048 tokens in documents of
-// 300, biased: 35 us; without documents and bias 46 us (0.56 PFLOP/s), 16 samples of it 140 (0.73).
+// 500 on average, biased: 33 .. 37 us; without documents and bias 46 us (0.56 PFLOP/s), 16 samples of it 140 (0.73).
 #ifndef SBP_LM_ATTENTION_FWD_H_
 #define SBP_LM_ATTENTION_FWD_H_
 
