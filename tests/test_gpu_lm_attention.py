@@ -271,3 +271,32 @@ def test_largest_cap(dtype):
     c = Case(1, 150, 2, 1, 64, dtype, seed=22, causal=True, cap=1024.0, spread=3.0)
     check_forward(c)
     check_backward(c, _keep(1, 150, 90, 22))
+
+
+@pytest.mark.parametrize("dtype,d,h,hk", [("bf16", 64, 2, 1), ("bf16", 128, 2, 2), ("bf16", 16, 3, 1), ("f32", 32, 1, 1)])
+def test_one_long_sample_is_its_documents(dtype, d, h, hk):
+    """17000 tokens in one sample (several lists of tiles) against the oracle on the 34 samples of 500 that its documents make."""
+    B, n = 34, 500
+    own = _docs(B, n, 23)
+    c = Case(B, n, h, hk, d, dtype, seed=23, causal=True, slopes=True, doc=own)
+    kw = dict(c.kw(), B=1, doc=(c.doc.view(B, n) + 1000 * torch.arange(B, dtype=torch.int32)[:, None]).reshape(-1).cuda())
+    check_forward(c, out=sbp.forward_attention_masked(c.qkv.cuda(), **kw))
+    check_backward(c, run=lambda q, A, g, l, idx: sbp.backward_attention_masked(q, A, g, l, **kw))
+    check_backward(c, _keep(B, n, 333, 23), run=lambda q, A, g, l, idx: sbp.backward_attention_masked(q, A, g, l, n=B * n, idx=idx, **kw))
+
+
+@pytest.mark.parametrize("d", [32, 128])
+@pytest.mark.parametrize("mods", [dict(causal=True), dict(causal=True, cap=20.0, prefix=[9000]), dict(slopes=True)])
+def test_long_samples_without_documents(d, mods):
+    """9500 tokens: bf16 against the fp32 kernels, which share no tile code.  A weight is off by 2^-8 as an operand, an output by 2^-8 as it is
+    stored, so A by at most 2^-7 of the weighted sum of |v| and 1 % of that for everything in fp32."""
+    c = Case(1, 9500, 2, 1, d, "bf16", seed=24, **mods)
+    kw, qkv = c.kw(), c.qkv.cuda()
+    A, lse = sbp.forward_attention_masked(qkv, **kw)
+    wide = qkv.float()
+    fA, fl = sbp.forward_attention_masked(wide, **kw)
+    wide[:, 3 * d:] = wide[:, 3 * d:].abs()
+    size, _ = sbp.forward_attention_masked(wide, **kw)
+    assert ((A.float() - fA).abs() <= 1.01 * 2.0 ** -7 * size).all()
+    # lse: the scores' (d + 8) 2^-23 scale |q||k| of each side (|q||k| below 4 d here), and the sum's 9500 2^-24 with slack for exponentials
+    assert ((lse - fl).abs() <= 2 * ((d + 8) * 4 * d * c.scale * 2.0 ** -23 + 9500 * 2.0 ** -22)).all()
