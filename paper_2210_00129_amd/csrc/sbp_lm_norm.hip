@@ -16,27 +16,46 @@ template <typename T> struct LmPiece;                      // 16 bytes of a row
 template <> struct LmPiece<float> { static constexpr int N = 4; };
 template <> struct LmPiece<uint16_t> { static constexpr int N = 8; };
 
-// The channels of a thread: pieces of 16 bytes (VEC), piece i at channel (i * TS + t) * N, or single channels i * TS + t.
-template <typename T, int TS, int E, bool VEC>
+// The channels of a thread: pieces of 16 bytes (PIECES), piece i at channel (i * TS + t) * N, or single channels i * TS + t.  VEC: the rows are
+// whole pieces at multiples of 16 bytes.  Pieces without VEC lie at any multiple of an element, and the last one of a row goes element by
+// element; that takes fewer addresses and more comparisons than single channels, and pays only where the registers are short: the backward
+// of more than 8192 channels (4096 x 12001, half of the rows kept, fp32 423 us, single channels 2878; bf16 277 and 439; but 16384 x 4095,
+// bf16, 243 and 175).
+template <typename T, int TS, int E, bool VEC, bool PIECES = VEC>
 struct LmRow {
-  static constexpr int N = VEC ? LmPiece<T>::N : 1, P = E / N;
+  static constexpr int N = PIECES ? LmPiece<T>::N : 1, P = E / N;
   static_assert(E % N == 0, "whole pieces");
   int t, C;
   __device__ __forceinline__ int channel(int i) const { return (i / N * TS + t) * N + i % N; }
-  __device__ __forceinline__ bool valid(int i) const { return (i / N * TS + t) * N < C; }   // (VEC: C is a multiple of N)
-  using Piece = typename std::conditional<VEC, uint4, T>::type;
+  __device__ __forceinline__ bool valid(int i) const { return (VEC ? (i / N * TS + t) * N : channel(i)) < C; }   // (VEC: C is a multiple of N)
+  using Piece = typename std::conditional<PIECES, uint4, T>::type;
   struct Raw { Piece p[P]; };                              // the thread's part of a row as it lies in memory (zeros past C)
   __device__ __forceinline__ void load(const T* row, Raw& w) const {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = (p * TS + t) * N;
-      w.p[p] = c < C ? *reinterpret_cast<const Piece*>(row + c) : Piece{};
+      if constexpr (VEC || !PIECES) {
+        w.p[p] = c < C ? *reinterpret_cast<const Piece*>(row + c) : Piece{};
+      } else {
+        uint32_t v[4] = {0, 0, 0, 0};
+        if (c + N <= C) {
+          __builtin_memcpy(v, row + c, 16);
+        } else if (c < C) {
+#pragma unroll
+          for (int e = 0; e < N - 1; ++e)
+            if (c + e < C) {
+              if constexpr (sizeof(T) == 4) v[e] = __float_as_uint(row[c + e]);
+              else v[e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
+            }
+        }
+        w.p[p] = make_uint4(v[0], v[1], v[2], v[3]);
+      }
     }
   }
   static __device__ __forceinline__ void widen(const Raw& w, float (&v)[E]) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      if constexpr (!VEC) {
+      if constexpr (!PIECES) {
         if constexpr (sizeof(T) == 4) v[p] = w.p[p];
         else v[p] = __uint_as_float((uint32_t)w.p[p] << 16);
       } else {
@@ -54,14 +73,28 @@ struct LmRow {
     for (int p = 0; p < P; ++p) {
       const int c = (p * TS + t) * N;
       if (c >= C) continue;
-      if constexpr (!VEC) {
+      if constexpr (!PIECES) {
         if constexpr (sizeof(T) == 4) row[c] = v[p];
         else row[c] = (uint16_t)bf16_pack(v[p], v[p]);
-      } else if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(row + c) = make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
       } else {
-        *reinterpret_cast<uint4*>(row + c) = make_uint4(bf16_pack(v[8 * p], v[8 * p + 1]), bf16_pack(v[8 * p + 2], v[8 * p + 3]),
-                                                        bf16_pack(v[8 * p + 4], v[8 * p + 5]), bf16_pack(v[8 * p + 6], v[8 * p + 7]));
+        uint32_t x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 4) x[e] = __float_as_uint(v[4 * p + e]);
+          else x[e] = bf16_pack(v[8 * p + 2 * e], v[8 * p + 2 * e + 1]);
+        }
+        if constexpr (VEC) {
+          *reinterpret_cast<uint4*>(row + c) = make_uint4(x[0], x[1], x[2], x[3]);
+        } else if (c + N <= C) {
+          __builtin_memcpy(row + c, x, 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < N - 1; ++e)
+            if (c + e < C) {
+              if constexpr (sizeof(T) == 4) row[c + e] = __uint_as_float(x[e]);
+              else row[c + e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
+            }
+        }
       }
     }
   }
@@ -222,7 +255,7 @@ struct LmNormBwd {
 template <typename T, int TS, int E, bool VEC, bool LAYER, bool SHIFT>
 __global__ void __launch_bounds__(LmTeams<TS>::THREADS) residual_norm_backward_kernel(LmNormBwd a) {
   constexpr int TEAMS = LmTeams<TS>::N, Q = SHIFT ? 4 : 2;
-  using Row = LmRow<T, TS, E, VEC>;
+  using Row = LmRow<T, TS, E, VEC, VEC || E == 16>;
   __shared__ float red[TS > 64 ? 8 * (TS / 64) : 1];
   int slot = 0;
   const int team = TEAMS > 1 ? threadIdx.x / TS : 0;
