@@ -255,7 +255,7 @@ struct LmNormBwd {
 template <typename T, int TS, int E, bool VEC, bool LAYER, bool SHIFT>
 __global__ void __launch_bounds__(LmTeams<TS>::THREADS) residual_norm_backward_kernel(LmNormBwd a) {
   constexpr int TEAMS = LmTeams<TS>::N, Q = SHIFT ? 4 : 2;
-  using Row = LmRow<T, TS, E, VEC, VEC || E == 16>;
+  using Row = LmRow<T, TS, E, VEC, VEC || (E == 16 && TS == 1024)>;
   __shared__ float red[TS > 64 ? 8 * (TS / 64) : 1];
   int slot = 0;
   const int team = TEAMS > 1 ? threadIdx.x / TS : 0;
@@ -516,11 +516,22 @@ template <typename T, bool LAYER, bool SHIFT>
 static void launch_norm_bwd(const LmNormBwd& a, bool vec, hipStream_t s) {
   const unsigned blocks = (unsigned)(a.row_blocks + a.drop_blocks);
   if (!blocks) return;
-  lm_for_team(lm_team(a.C), [&](auto ts, auto e) {
+  auto go = [&](auto ts, auto e, auto v) {
     constexpr int TS = decltype(ts)::value, E = decltype(e)::value;
-    const dim3 block(LmTeams<TS>::THREADS);
-    if (vec) SBP_LAUNCH(SBP_PROF_OTHER, s, (residual_norm_backward_kernel<T, TS, E, true, LAYER, SHIFT>), dim3(blocks), block, 0, s, a);
-    else SBP_LAUNCH(SBP_PROF_OTHER, s, (residual_norm_backward_kernel<T, TS, E, false, LAYER, SHIFT>), dim3(blocks), block, 0, s, a);
+    SBP_LAUNCH(SBP_PROF_OTHER, s, (residual_norm_backward_kernel<T, TS, E, decltype(v)::value, LAYER, SHIFT>), dim3(blocks), dim3(LmTeams<TS>::THREADS), 0, s, a);
+  };
+  // 1024 threads have 128 registers each: rows of 4097 .. 8192 channels go to 512 threads of 16 channels where that saves enough of them (bf16,
+  // 16384 x 8192: 247 -> 224 us; layer norms with betas, 8192 x 5120: 224 -> 109), not where single channels need many addresses besides
+  // (16384 x 8191: 351, 388 so)
+  const int team = lm_team(a.C);
+  if (team == 1024 && (vec || SHIFT)) {
+    if (vec) go(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{}, std::true_type{});
+    else if constexpr (SHIFT) go(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{}, std::false_type{});
+    return;
+  }
+  lm_for_team(team, [&](auto ts, auto e) {
+    if (vec) go(ts, e, std::true_type{});
+    else go(ts, e, std::false_type{});
   });
 }
 

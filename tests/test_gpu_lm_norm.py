@@ -249,3 +249,20 @@ def test_offsets_beyond_32_bits():
                                     flags=sbp.FLAG_DX_COMPACT)
     assert torch.equal(g1["dx"][-5:], g2["dx"]) and torch.equal(g1["dy_k"], g2["dy_k"])
     assert (g1["dx"][:-5] == 0).all()
+
+
+@pytest.mark.parametrize("M,C,G", [(7, 5001, 1), (6, 8191, 3), (5, 8184, 1), (4, 12001, 2), (10, 1031, 1), (9, 640, 1)])
+@pytest.mark.parametrize("kind", [sbp.NORM_RMS, sbp.NORM_LAYER])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_backward_without_the_gradients_of_the_betas(M, C, G, kind, dtype):
+    """The sums of dz and t are left out where nothing asks for them (other kernels)."""
+    c = Norms(M, C, dtype, kind, post=True, pre=True, beta=False, G=G, alpha=0.7, seed=31)
+    idx = _kept(c, 0.6, 31)
+    got, ref, want = _backward(c, idx)
+    _check(c, got, ref, want, len(idx))
+    at = torch.from_numpy(idx).long()
+    few = [w for w in want if "beta" not in w]
+    again = sbp.backward_residual_norm(c.d_out.cuda(), c.dz[at].cuda(), c.x[at].cuda(), c.y[at].cuda(), torch.from_numpy(idx).cuda(), c.M, want=few,
+                                       **c.kw(True, beta_pre=False))
+    assert sorted(again) == sorted(few)
+    _check(c, again, ref, few, len(idx))
