@@ -523,15 +523,17 @@ static void launch_norm_bwd(const LmNormBwd& a, bool vec, hipStream_t s) {
   // 1024 threads have 128 registers each: rows of 4097 .. 8192 channels go to 512 threads of 16 channels where that saves enough of them (bf16,
   // 16384 x 8192: 247 -> 224 us; layer norms with betas, 8192 x 5120: 224 -> 109), not where single channels need many addresses besides
   // (16384 x 8191: 351, 388 so)
-  const int team = lm_team(a.C);
-  if (team == 1024 && (vec || SHIFT)) {
-    if (vec) go(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{}, std::true_type{});
-    else if constexpr (SHIFT) go(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{}, std::false_type{});
-    return;
-  }
-  lm_for_team(team, [&](auto ts, auto e) {
-    if (vec) go(ts, e, std::true_type{});
-    else go(ts, e, std::false_type{});
+  lm_for_team(lm_team(a.C), [&](auto ts, auto e) {
+    if constexpr (decltype(ts)::value == 1024 && decltype(e)::value == 8) {
+      constexpr std::integral_constant<int, 512> half{};
+      constexpr std::integral_constant<int, 16> twice{};
+      if (vec) go(half, twice, std::true_type{});
+      else if constexpr (SHIFT) go(half, twice, std::false_type{});
+      else go(ts, e, std::false_type{});
+    } else {
+      if (vec) go(ts, e, std::true_type{});
+      else go(ts, e, std::false_type{});
+    }
   });
 }
 
