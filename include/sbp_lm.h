@@ -4,7 +4,8 @@
  * types, flags and status codes as sbp.h: device pointers, dense row-major tensors, nothing allocated, arguments
  * validated on the host before the first HIP call, outputs fully overwritten unless a flag says otherwise, calls only
  * enqueue work on `stream`.  Every call may be captured into a HIP graph.  A call runs on the current device, which must be the one that
- * holds its tensors.
+ * holds its tensors.  Outputs and workspaces share no memory with an input or with each other, except where an output may be an input
+ * itself; calls that break this are refused (SBP_ERR_SHAPE).
  */
 #ifndef SBP_LM_H_
 #define SBP_LM_H_

@@ -1,6 +1,7 @@
 // C ABI of the language-model steps (sbp_lm.h): host-side validation, then kernel launches.  Every argument check runs before
 // the first HIP call, so that error paths need no device.
 #include <cmath>
+#include <initializer_list>
 
 #include "sbp_lm_internal.h"
 
@@ -14,6 +15,29 @@ static int32_t check_workspace(const void* ws, size_t have, size_t need) {
     return fail(SBP_ERR_WORKSPACE, "workspace missing, misaligned or smaller than %zu bytes", need);
   return SBP_OK;
 }
+
+// A tensor of a call; an output may be one of two inputs itself (`same`), element for element.
+struct Range {
+  const char* name;
+  const void* p;
+  size_t bytes;
+  const void* same[2] = {nullptr, nullptr};
+};
+static bool overlap(const Range& a, const Range& b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return x && y && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+// Outputs (the workspace is one) share no memory with an input nor with each other: the workgroups of a launch run in any order.
+static int32_t check_overlap(std::initializer_list<Range> outs, std::initializer_list<Range> ins) {
+  for (const Range* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Range& i : ins)
+      if (overlap(*o, i) && !(o->p == i.p && (o->p == o->same[0] || o->p == o->same[1]))) return fail(SBP_ERR_SHAPE, "%s and %s overlap", o->name, i.name);
+    for (const Range* q = outs.begin(); q != o; ++q)
+      if (overlap(*o, *q)) return fail(SBP_ERR_SHAPE, "%s and %s overlap", o->name, q->name);
+  }
+  return SBP_OK;
+}
+static size_t elem_bytes(int32_t dtype) { return dtype == SBP_F32 ? 4 : 2; }
 
 // rows: tokens per sample in the tensors
 static int32_t validate_masked(const sbp_attention_desc* a, int64_t rows, int32_t dtype) {
@@ -94,11 +118,16 @@ using namespace sbp;
 extern "C" {
 
 int32_t sbp_forward_attention_masked(const sbp_attention_desc* desc, const void* qkv, int32_t dtype, void* A, float* lse, void* stream) {
-  const int32_t st = validate_masked(desc, 0, dtype);
+  int32_t st = validate_masked(desc, 0, dtype);
   if (st != SBP_OK) return st;
   if (!qkv || !A) return fail(SBP_ERR_NULL, "qkv or A is NULL");
   if (((uintptr_t)qkv | (uintptr_t)A) & 15) return fail(SBP_ERR_SHAPE, "tensors must be 16-byte aligned");
   if (A == qkv) return fail(SBP_ERR_SHAPE, "A must not be qkv");
+  const size_t rows = (size_t)desc->B * desc->n, size = elem_bytes(dtype);
+  st = check_overlap({{"A", A, rows * desc->h * desc->d * size}, {"lse", lse, rows * desc->h * 4}},
+                     {{"qkv", qkv, rows * (desc->h + 2 * (size_t)desc->h_kv) * desc->d * size}, {"slopes", desc->slopes, (size_t)desc->h * 4},
+                      {"doc", desc->doc, rows * 4}, {"prefix", desc->prefix, (size_t)desc->B * 4}});
+  if (st != SBP_OK) return st;
   MaskedAttention a = masked_args(*desc, desc->n);
   a.qkv = qkv; a.out = A; a.lse_out = lse;
   return launch_forward_attention_masked(a, dtype, static_cast<hipStream_t>(stream));
@@ -121,6 +150,13 @@ int32_t sbp_backward_attention_masked(const sbp_attention_desc* desc, const void
   const MaskedAttentionPlan p = plan_masked_attention_backward(*desc, n_k, dtype);
   st = check_workspace(ws, ws_bytes, p.bytes);
   if (st != SBP_OK) return st;
+  const size_t rows = (size_t)desc->B * n_k, size = elem_bytes(dtype), out = rows * desc->h * desc->d * size,
+               all = rows * (desc->h + 2 * (size_t)desc->h_kv) * desc->d * size;
+  st = check_overlap({{"dqkv_k", dqkv_k, all}, {"the workspace", ws, p.bytes}},
+                     {{"qkv_k", qkv_k, all}, {"A_k", A_k, out}, {"dA_k", dA_k, out}, {"lse_k", lse_k, rows * desc->h * 4}, {"idx", idx, rows * 4},
+                      {"slopes", desc->slopes, (size_t)desc->h * 4}, {"doc", desc->doc, (size_t)desc->B * desc->n * 4},
+                      {"prefix", desc->prefix, (size_t)desc->B * 4}});
+  if (st != SBP_OK) return st;
   MaskedAttention a = masked_args(*desc, n_k);
   a.qkv = qkv_k; a.A = A_k; a.dA = dA_k; a.lse = lse_k; a.idx = idx; a.out = dqkv_k;
   return launch_backward_attention_masked(a, p, dtype, ws, static_cast<hipStream_t>(stream));
@@ -128,13 +164,18 @@ int32_t sbp_backward_attention_masked(const sbp_attention_desc* desc, const void
 
 int32_t sbp_forward_residual_norm(const sbp_residual_norm_desc* desc, const void* x, const void* y, int32_t dtype, void* x_out, void* z,
                                   void* stream) {
-  const int32_t st = validate_residual(desc, dtype);
+  int32_t st = validate_residual(desc, dtype);
   if (st != SBP_OK) return st;
   if (!x) return fail(SBP_ERR_NULL, "x is NULL");
   if (!y && (desc->gate || desc->gamma_post)) return fail(SBP_ERR_NULL, "y is NULL but gate or gamma_post is given");
   if (z && !desc->gamma_pre) return fail(SBP_ERR_NULL, "gamma_pre is NULL but z is requested");
   if (z && (z == x || z == y || z == x_out)) return fail(SBP_ERR_SHAPE, "z must be a buffer of its own");
   if (!x_out && !z) return SBP_OK;
+  const size_t all = (size_t)desc->M * desc->C * elem_bytes(dtype), c = (size_t)desc->C * 4;
+  st = check_overlap({{"x_out", x_out, all, {x, y}}, {"z", z, all}},
+                     {{"x", x, all}, {"y", y, all}, {"gate", desc->gate, desc->G * c}, {"gamma_post", desc->gamma_post, c}, {"beta_post", desc->beta_post, c},
+                      {"gamma_pre", desc->gamma_pre, c}, {"beta_pre", desc->beta_pre, c}});
+  if (st != SBP_OK) return st;
   return launch_forward_residual_norm(*desc, x, y, dtype, x_out, z, static_cast<hipStream_t>(stream));
 }
 
@@ -162,17 +203,27 @@ int32_t sbp_backward_residual_norm(const sbp_residual_norm_desc* desc, const voi
   const ResidualNormPlan p = plan_residual_norm_backward(*desc, K, dtype, flags);
   st = check_workspace(ws, ws_bytes, p.bytes);
   if (st != SBP_OK) return st;
+  const size_t c = (size_t)desc->C * 4, kept = (size_t)K * desc->C * elem_bytes(dtype), all = compact ? kept : (size_t)desc->M * desc->C * elem_bytes(dtype);
+  st = check_overlap({{"dx", dx, all, {dx_out, nullptr}}, {"dy_k", dy_k, kept, {y_k, dz_k}}, {"dgate", g.dgate, desc->G * c}, {"dgamma_post", g.dgamma_post, c},
+                      {"dbeta_post", g.dbeta_post, c}, {"dgamma_pre", g.dgamma_pre, c}, {"dbeta_pre", g.dbeta_pre, c}, {"the workspace", ws, p.bytes}},
+                     {{"dx_out", dx_out, all}, {"dz_k", dz_k, kept}, {"x_out_k", x_out_k, kept}, {"y_k", y_k, kept}, {"idx", compact ? nullptr : idx, (size_t)K * 4},
+                      {"inv", compact ? nullptr : inv, (size_t)desc->M * 4}, {"gate", desc->gate, desc->G * c}, {"gamma_post", desc->gamma_post, c},
+                      {"beta_post", desc->beta_post, c}, {"gamma_pre", desc->gamma_pre, c}, {"beta_pre", desc->beta_pre, c}});
+  if (st != SBP_OK) return st;
   return launch_backward_residual_norm(p, *desc, dx_out, dz_k, x_out_k, y_k, idx, inv, K, dtype, dx, dy_k, g, ws, flags,
                                        static_cast<hipStream_t>(stream));
 }
 
 int32_t sbp_forward_embedding(const void* tokens, int32_t token_bytes, const void* table, int64_t M, int64_t V, int32_t C, float scale,
                               int32_t dtype, void* E, void* stream) {
-  const int32_t st = validate_embedding(M, V, C, scale, token_bytes, dtype);
+  int32_t st = validate_embedding(M, V, C, scale, token_bytes, dtype);
   if (st != SBP_OK) return st;
   if (M == 0) return SBP_OK;
   if (!tokens || !table || !E) return fail(SBP_ERR_NULL, "tokens, table or E is NULL");
   if ((uintptr_t)tokens % token_bytes) return fail(SBP_ERR_SHAPE, "tokens must be aligned to their size");
+  const size_t row = (size_t)C * elem_bytes(dtype);
+  st = check_overlap({{"E", E, M * row}}, {{"tokens", tokens, (size_t)M * token_bytes}, {"table", table, V * row}});
+  if (st != SBP_OK) return st;
   return launch_forward_embedding(tokens, token_bytes, table, M, V, C, scale, dtype, E, static_cast<hipStream_t>(stream));
 }
 
@@ -192,6 +243,10 @@ int32_t sbp_backward_embedding(const void* dE, const void* tokens, int32_t token
   if ((uintptr_t)tokens % token_bytes) return fail(SBP_ERR_SHAPE, "tokens must be aligned to their size");
   const EmbeddingPlan p = plan_embedding_backward(K, V, C, flags);
   st = check_workspace(ws, ws_bytes, p.bytes);
+  if (st != SBP_OK) return st;
+  st = check_overlap({{"dtable", dtable, (size_t)V * C * (flags & SBP_FLAG_DW_OUT_BF16 ? 2 : 4)}, {"the workspace", ws, p.bytes}},
+                     {{"dE", dE, (size_t)(flags & SBP_FLAG_DY_COMPACT ? K : M) * C * elem_bytes(dtype)}, {"tokens", tokens, (size_t)M * token_bytes},
+                      {"idx", idx, (size_t)K * 4}});
   if (st != SBP_OK) return st;
   return launch_backward_embedding(p, dE, tokens, token_bytes, idx, M, K, V, C, scale, dtype, dtable, ws, flags,
                                    static_cast<hipStream_t>(stream));
