@@ -48,6 +48,7 @@ typedef struct sbp_attention_desc {
   const int32_t* doc;     /* device, [B*n] document of every token (any numbers; < 0: of none), or NULL */
   const int32_t* prefix;  /* device, [B] keys at positions below it are visible to all queries of the sample (within the
                              document); only with causal = 1; or NULL */
+  /* one call: B * n < 2^31, (h + 2*h_kv) * d <= 2^24, B * h * ceil(n / 32) < 2^22 */
 } sbp_attention_desc;
 
 /*

@@ -50,7 +50,8 @@ static int32_t validate_masked(const sbp_attention_desc* a, int64_t rows, int32_
   if ((a->h + 2LL * a->h_kv) * a->d > (1 << 24)) return fail(SBP_ERR_SHAPE, "(h + 2 h_kv) * d is too large");
   if (a->n > (1 << 24)) return fail(SBP_ERR_SHAPE, "n=%d: positions beyond 2^24 are not exact in fp32", a->n);
   if (rows < 0 || rows > a->n) return fail(SBP_ERR_SHAPE, "need 0 <= n_k <= n, got n_k=%lld n=%d", (long long)rows, a->n);
-  // (a grid of 256 or 512 threads per 32 tokens and head, in two roles, stays below 2^32 threads)
+  // (a grid of 256 or 512 threads per 32 tokens and head, in two roles, stays below 2^32 threads; and the four tables of the backward's
+  // workspace, 4 bytes per token and head of samples padded to 64 tokens, below 2^32 bytes together: its kernel's offsets into them are 32 bits)
   if ((int64_t)a->B * a->h * ceil_div(a->n, 32) >= (1 << 22)) return fail(SBP_ERR_SHAPE, "B * h * n is too large for one call");
   if (a->causal != 0 && a->causal != 1) return fail(SBP_ERR_FLAGS, "causal must be 0 or 1, got %d", a->causal);
   if (!std::isfinite(a->scale)) return fail(SBP_ERR_SHAPE, "scale must be finite");

@@ -253,7 +253,8 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
         if constexpr (KEY) st2.issue(dA + head * D, t0, rows, buf + F::S::IMG, lane, wave);
         else st1.issue(qkv + (a.h + a.hk + kv) * D, t0, rows, buf + F::S::IMG, lane, wave);
         if (wave == 3) {
-          // (the tables lie within 2^31 bytes of each other)
+          // (every place in the tables is less than 2^32 bytes behind l2, and the copies take their offsets as unsigned: the limit on
+          // B h n / 32 leaves each of the four tables less than 2^30 bytes)
           const uint32_t th = 4u * (uint32_t)((b * a.h + head) * w.npad + t0), tb = 4u * (uint32_t)(b * w.npad + t0);
           lm_copy16(w.l2, table_off + (lane < 32 ? th : tb), buf + F::TABLE);
         }
