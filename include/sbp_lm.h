@@ -150,6 +150,7 @@ int32_t sbp_backward_residual_norm(const sbp_residual_norm_desc* desc, const voi
  * Token table.  Forward: E[r, :] = scale * table[tokens[r], :], rounded once; a token outside [0, V) gives a row of +0.
  *   tokens  device, in, [M] int32 (token_bytes = 4) or int64 (token_bytes = 8)
  *   table   device, in, [V, C] of `dtype`;   E  device, out, [M, C] of `dtype`
+ * M < 2^31, V < 2^30, C <= 2^30.
  */
 int32_t sbp_forward_embedding(const void* tokens, int32_t token_bytes, const void* table, int64_t M, int64_t V, int32_t C,
                               float scale, int32_t dtype, void* E, void* stream);
@@ -169,7 +170,7 @@ size_t sbp_backward_embedding_workspace(int64_t M, int64_t K, int64_t V, int32_t
  *           also the output projection's weight)
  *   flags   SBP_FLAG_DY_COMPACT, SBP_FLAG_ACCUMULATE_DW, SBP_FLAG_DW_OUT_BF16
  *   workspace  device, 256-byte aligned, sbp_backward_embedding_workspace(...) bytes
- * K < 2^30, V < 2^30, K * C < 2^37.
+ * K < 2^30, V < 2^30, C <= 2^30, K * C < 2^37.
  */
 int32_t sbp_backward_embedding(const void* dE, const void* tokens, int32_t token_bytes, const int32_t* idx, int64_t M, int64_t K,
                                int64_t V, int32_t C, float scale, int32_t dtype, void* dtable, void* workspace,

@@ -98,6 +98,8 @@ static int32_t validate_embedding(int64_t M, int64_t V, int32_t C, float scale, 
   if (!known_dtype(dtype)) return fail(SBP_ERR_DTYPE, "unknown dtype %d", dtype);
   if (token_bytes != 4 && token_bytes != 8) return fail(SBP_ERR_DTYPE, "token_bytes must be 4 or 8, got %d", token_bytes);
   if (M < 0 || M > INT32_MAX || V < 1 || V >= (1 << 30) || C < 1) return fail(SBP_ERR_SHAPE, "bad shape M=%lld V=%lld C=%d", (long long)M, (long long)V, C);
+  // (a lane's next column, up to 2048 on, and a slice's end stay below 2^31)
+  if (C > (1 << 30)) return fail(SBP_ERR_SHAPE, "C=%d is larger than 2^30", C);
   if (!std::isfinite(scale)) return fail(SBP_ERR_SHAPE, "scale must be finite");
   return SBP_OK;
 }

@@ -184,11 +184,15 @@ PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+int32_t channels(int64_t C) {
+  if (C != (int32_t)C) fail(PyExc_ValueError, "%s", "too many channels");
+  return (int32_t)C;
+}
+
 // a: gate, alpha, gamma_post, beta_post, gamma_pre, beta_pre, kind, eps
 sbp_residual_norm_desc norm_desc(PyObject* const* a, int64_t M, int64_t C, c10::Device device) {
   sbp_residual_norm_desc d{};
-  if (C != (int32_t)C) fail(PyExc_ValueError, "%s", "too many channels");
-  d.M = M; d.C = (int32_t)C; d.G = 1;
+  d.M = M; d.C = channels(C); d.G = 1;
   const at::Tensor* gate = tensor(a[0], "gate");
   if (gate && gate->dim() == 1) {
     d.gate = address<const float>(gate, "gate", {C}, at::kFloat, device);
@@ -325,7 +329,8 @@ PyObject* embedding_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &tokens = needed(a[0], "tokens"), &table = matrix(a[1], "table");
     const int32_t code = dtype_code(table);
     const c10::Device device = table.device();
-    const int64_t V = table.size(0), C = table.size(1);
+    const int64_t V = table.size(0);
+    const int32_t C = channels(table.size(1));
     int32_t bytes;
     const void* tp = token_address(tokens, device, &bytes);
     const void* p = address(&table, "table", {V, C}, table.scalar_type(), device);
@@ -335,7 +340,7 @@ PyObject* embedding_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* out = address(or_new(tensor(a[3], "out"), made, shape, table.scalar_type(), device), "out", shape, table.scalar_type(), device);
     const float scale = number(a[2]);
     const int64_t M = tokens.numel();
-    run(device, [&](void* s) { return f_emb(tp, bytes, p, M, V, (int32_t)C, scale, code, out, s); });
+    run(device, [&](void* s) { return f_emb(tp, bytes, p, M, V, C, scale, code, out, s); });
     return keep_or_wrap(a[3], made);
   } catch (const PyFail&) { return nullptr; }
   END_HANDLE_TH_ERRORS
@@ -350,7 +355,8 @@ PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor* idx = tensor(a[3], "idx");
     const int32_t code = dtype_code(dE);
     const c10::Device device = dE.device();
-    const int64_t V = integer(a[2], true), C = dE.size(1), M = tokens.numel(), K = idx ? idx->numel() : M;
+    const int64_t V = integer(a[2], true), M = tokens.numel(), K = idx ? idx->numel() : M;
+    const int32_t C = channels(dE.size(1));
     const uint32_t flags = (uint32_t)bits64(a[5], true);
     if (V < 0) fail(PyExc_ValueError, "%s", "V must not be negative");
     int32_t bytes;
@@ -363,8 +369,8 @@ PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::Tensor made;
     void* out = address(or_new(given, made, {V, C}, type, device), "dtable", {V, C}, type, device);
     const float scale = number(a[4]);
-    const Workspace ws(a[7], f_emb_bwd_ws(M, K, V, (int32_t)C, code, flags), device);
-    run(device, [&](void* s) { return f_emb_bwd(p, tp, bytes, ip, M, K, V, (int32_t)C, scale, code, out, ws.p, ws.bytes, flags, s); });
+    const Workspace ws(a[7], f_emb_bwd_ws(M, K, V, C, code, flags), device);
+    run(device, [&](void* s) { return f_emb_bwd(p, tp, bytes, ip, M, K, V, C, scale, code, out, ws.p, ws.bytes, flags, s); });
     return keep_or_wrap(a[6], made);
   } catch (const PyFail&) { return nullptr; }
   END_HANDLE_TH_ERRORS

@@ -1,0 +1,15 @@
+"""What the Python calls of the language-model steps refuse because a number does not fit the field that it goes into."""
+import pytest
+import torch
+
+import paper_2210_00129_amd as sbp
+
+pytestmark = pytest.mark.gpu
+
+
+def test_channels_beyond_32_bits():
+    """(a view of one element: nothing of this size is allocated)"""
+    wide, tok = torch.zeros(1, 1, dtype=torch.bfloat16, device="cuda").expand(1, (1 << 32) + 8), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for call in (lambda: sbp.forward_embedding(tok, wide), lambda: sbp.backward_embedding(wide, tok, 5), lambda: sbp.forward_residual_norm(wide)):
+        with pytest.raises(ValueError, match="too many channels"):
+            call()

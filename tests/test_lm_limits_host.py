@@ -25,3 +25,13 @@ def test_attention_refuses_more():
         d = _lib.AttentionDesc(B, n, h, h, 16, 1, 0.25, 0.0, None, None, None)
         assert _lib.lib().sbp_backward_attention_masked_workspace(d, n, 1) == 0
         assert _lib.lib().sbp_forward_attention_masked(d, 4096, 1, 1 << 20, None, None) == SHAPE
+
+
+def test_table_refuses_more_channels_than_its_kernels_count():
+    """A lane's next column is an int: beyond 2^30 channels a step of 2048 would pass 2^31."""
+    L = _lib.lib()
+    for C in ((1 << 30) + 1, (1 << 31) - 1):
+        assert L.sbp_forward_embedding(4096, 4, 1 << 40, 1, 1, C, 1.0, 1, 1 << 45, None) == SHAPE
+        assert L.sbp_backward_embedding_workspace(300, 300, 1, C, 1, 0) == 0
+        assert L.sbp_backward_embedding(1 << 40, 4096, 4, None, 1, 1, 1, C, 1.0, 1, 1 << 45, None, 0, 0, None) == SHAPE
+    assert L.sbp_backward_embedding_workspace(300, 300, 1, 1 << 28, 1, 0) > 0
