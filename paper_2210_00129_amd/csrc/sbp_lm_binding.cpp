@@ -29,6 +29,12 @@ int32_t number32(PyObject* o) {
   if (v != (int32_t)v) fail(PyExc_ValueError, "%s", "a size is beyond 32 bits");
   return (int32_t)v;
 }
+// flags: 32 bits, and refused where one is set beyond them
+uint32_t flags32(PyObject* o) {
+  const uint64_t v = bits64(o, true);
+  if (v >> 32) fail(PyExc_ValueError, "%s", "unknown flags beyond 32 bits");
+  return (uint32_t)v;
+}
 bool truth(PyObject* o) {
   const int v = PyObject_IsTrue(o);
   if (v < 0) throw PyFail{};
@@ -251,7 +257,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t C = some.size(1), M = integer(a[5], true);
     const c10::Device device = some.device();
     const at::ScalarType type = some.scalar_type();
-    const uint32_t flags = (uint32_t)bits64(a[15], true);
+    const uint32_t flags = flags32(a[15]);
     const bool compact = flags & SBP_FLAG_DX_COMPACT;
     const int64_t K = idx ? idx->numel() : some.size(0), rows = compact ? K : M;
     const sbp_residual_norm_desc d = norm_desc(a + 6, M, C, device);
@@ -357,7 +363,7 @@ PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const c10::Device device = dE.device();
     const int64_t V = integer(a[2], true), M = tokens.numel(), K = idx ? idx->numel() : M;
     const int32_t C = channels(dE.size(1));
-    const uint32_t flags = (uint32_t)bits64(a[5], true);
+    const uint32_t flags = flags32(a[5]);
     if (V < 0) fail(PyExc_ValueError, "%s", "V must not be negative");
     int32_t bytes;
     const void* tp = token_address(tokens, device, &bytes);

@@ -13,3 +13,12 @@ def test_channels_beyond_32_bits():
     for call in (lambda: sbp.forward_embedding(tok, wide), lambda: sbp.backward_embedding(wide, tok, 5), lambda: sbp.forward_residual_norm(wide)):
         with pytest.raises(ValueError, match="too many channels"):
             call()
+
+
+@pytest.mark.parametrize("flags", [1 << 32, 1 << 63, -1])
+def test_flags_beyond_32_bits(flags):
+    x, tok = torch.zeros(4, 8, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="flags"):
+        sbp.backward_embedding(x, tok, 5, flags=flags)
+    with pytest.raises(ValueError, match="flags"):
+        sbp.backward_residual_norm(x, None, None, x, tok, 4, flags=flags)
