@@ -240,6 +240,12 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// what a caller's container lent: it may lose the object while a lookup runs Python code or other threads run
+struct Held {
+  PyObject* o[7] = {};
+  ~Held() { for (PyObject* p : o) Py_XDECREF(p); }
+};
+
 const char* const kOutputs[7] = {"dx", "dy_k", "dgate", "dgamma_post", "dbeta_post", "dgamma_pre", "dbeta_pre"};
 
 // (dx_out, dz_k, x_out_k, y_k, idx, M, gate, alpha, gamma_post, beta_post, gamma_pre, None, kind, eps, inv, flags, want, dx, dy_k, grads,
@@ -288,11 +294,14 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* idx_p = address<const int32_t>(idx, "idx", {K}, at::kInt, device);
     const int32_t* inv_p = address<const int32_t>(inv, "inv", {M}, at::kInt, device);
     PyObject* given[7] = {a[17], a[18], Py_None, Py_None, Py_None, Py_None, Py_None};
+    Held held;
     if (a[19] != Py_None) {
       if (!PyDict_Check(a[19])) fail(PyExc_TypeError, "%s", "grads must be a dict");
       for (int q = 2; q < 7; ++q) {
         PyObject* g = PyDict_GetItemString(a[19], kOutputs[q]);
-        if (g) given[q] = g;
+        if (!g) continue;
+        Py_INCREF(g);
+        given[q] = held.o[q] = g;
       }
     }
     at::Tensor made[7];

@@ -22,3 +22,25 @@ def test_flags_beyond_32_bits(flags):
         sbp.backward_embedding(x, tok, 5, flags=flags)
     with pytest.raises(ValueError, match="flags"):
         sbp.backward_residual_norm(x, None, None, x, tok, 4, flags=flags)
+
+
+def test_gradients_that_leave_their_dict_during_the_call():
+    """The dict of preallocated gradients gives up one of them while the next is looked up (a key of the same hash, whose comparison
+    empties the entry): the call still owns what it took."""
+    M, C = 6, 40
+    x, idx = torch.randn(M, C, device="cuda"), torch.arange(M, dtype=torch.int32, device="cuda")
+    gamma, gate = torch.ones(C, device="cuda"), torch.ones(C, device="cuda")
+    args = dict(gate=gate, gamma_post=gamma, want=("dgate", "dgamma_post"))
+    want = sbp.backward_residual_norm(x, None, None, x, idx, M, **args)
+
+    class Taker(str):
+        def __hash__(self):
+            return hash("dgamma_post")
+
+        def __eq__(self, other):
+            grads.pop("dgate", None)
+            return False
+    grads = {Taker("taker"): None, "dgate": torch.empty(C, device="cuda")}
+    got = sbp.backward_residual_norm(x, None, None, x, idx, M, grads=grads, **args)
+    assert "dgate" not in grads
+    assert torch.equal(got["dgate"], want["dgate"]) and torch.equal(got["dgamma_post"], want["dgamma_post"])
