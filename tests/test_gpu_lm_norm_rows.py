@@ -1,5 +1,5 @@
-"""GPU parity of the step between two blocks, held to bounds that do not grow with the channels (lm_bounds),
-at every number of channels."""
+"""GPU parity of the step between two blocks, held to bounds that do not grow with the channels (lm_bounds): more rows than the launch has
+teams, so that every team takes several, crosses groups of the gate and adds up its rows; every number of channels."""
 import pytest
 import torch
 
@@ -39,6 +39,39 @@ def _check_backward(c, idx, flags=0, shift=False):
         dropped = torch.ones(c.M, dtype=torch.bool, device="cuda")
         dropped[idx] = False
         assert torch.equal(got["dx"][dropped], (c.alpha * c.d_out[dropped].float()).to(DT[c.dtype]))
+
+
+# rows, channels, gates: a team of the forward has 2048 (8192 up to 512 channels) others
+FORWARD = [(20000, 96, 5), (9000, 520, 3), (5000, 1030, 1), (4500, 2056, 2), (4300, 4100, 0), (4200, 8192, 1), (4200, 8200, 2), (2300, 12001, 1), (2100, 16384, 3)]
+
+
+@pytest.mark.parametrize("M,C,G", FORWARD)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_forward_of_several_rows_per_team(M, C, G, kind, dtype):
+    _check_forward(NormCase(M, C, dtype, kind, G=G, seed=C))
+
+
+# rows, channels, gates, kept rows per group: a team has 1023 (4095 up to 512 channels) to 255 others, split over the groups
+BACKWARD = [(20000, 96, 5, 1900), (9000, 520, 3, 2100), (5000, 1030, 1, 2600), (3200, 2056, 2, 750), (2600, 4096, 1, 1300), (1400, 5000, 0, 640),
+            (1200, 8184, 3, 190), (1400, 8191, 1, 650), (1400, 12001, 2, 300), (1300, 16384, 1, 600)]
+
+
+@pytest.mark.parametrize("M,C,G,per_group", BACKWARD)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("beta", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_backward_of_several_rows_per_team(M, C, G, per_group, kind, beta, dtype):
+    c = NormCase(M // max(G, 1) * max(G, 1), C, dtype, kind, beta=beta, G=G, seed=C)
+    _check_backward(c, c.kept(per_group))
+
+
+@pytest.mark.parametrize("M,C,K", [(300000, 64, 5), (40000, 1030, 7), (20000, 4100, 3), (18000, 8192, 2), (17000, 8200, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_runs_of_dropped_rows(M, C, K, dtype):
+    """More than 64 dropped rows for every team that passes them through."""
+    c = NormCase(M, C, dtype, NORM_LAYER, G=0, seed=C)
+    _check_backward(c, c.kept(K))
 
 
 CHANNELS = [1, 7, 64, 96, 200, 512, 513, 768, 771, 1024, 1030, 2048, 2056, 4096, 4104, 5000, 8184, 8191, 8192, 8200, 12001, 16383, 16384]
