@@ -1,5 +1,5 @@
 """GPU parity of the step between two blocks, held to bounds that do not grow with the channels (lm_bounds): more rows than the launch has
-teams, so that every team takes several, crosses groups of the gate and adds up its rows; every number of channels."""
+teams, so that every team takes several, crosses groups of the gate and adds up its rows; every number of channels; odd addresses."""
 import pytest
 import torch
 
@@ -87,3 +87,15 @@ def test_every_number_of_channels(C, kind, dtype, post, pre, beta, G):
     idx = c.kept(5)
     _check_backward(c, idx)
     _check_backward(c, idx, flags=sbp.FLAG_DX_COMPACT)
+
+
+@pytest.mark.parametrize("C", [136, 640, 1032, 2056, 5000, 8184, 12000, 16384])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_whole_vectors_at_odd_addresses(C, kind, dtype):
+    c = NormCase(24, C, dtype, kind, G=2, seed=C)
+    x = _shifted(c.x)
+    _check_forward(c, x=x, y=_shifted(c.y), x_out=_shifted(c.x), z=_shifted(c.x))
+    idx = c.kept(5)
+    _check_backward(c, idx, shift=True)
+    _check_backward(c, idx, flags=sbp.FLAG_DX_COMPACT, shift=True)
