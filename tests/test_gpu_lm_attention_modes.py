@@ -1,0 +1,30 @@
+"""GPU parity of the masked attention where the scores' arithmetic takes another of its kernels: scales of zero and below, caps above
+those whose weights need no maximum."""
+import numpy as np
+import pytest
+
+from lm_attention_gpu import Long
+from lm_util import Case, check_backward, check_forward
+
+pytestmark = pytest.mark.gpu
+
+
+def _keep(n, nk, seed):
+    return np.sort(np.random.default_rng(seed).choice(n, size=nk, replace=False))[None]
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.125, -1.5, 1e-30, -1e-30])
+@pytest.mark.parametrize("mods", [dict(), dict(causal=True), dict(causal=True, cap=20.0), dict(causal=True, cap=90.0), dict(slopes=True), dict(cap=3.0, slopes=True)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scales_of_zero_and_below(scale, mods, dtype):
+    for n, d, h, hk in ((150, 64, 2, 1), (200, 128, 2, 2), (70, 16, 2, 1)):
+        c = Case(1, n, h, hk, d, dtype, seed=31, scale=scale, **mods)
+        check_forward(c)
+        check_backward(c, _keep(n, n // 2, 31))
+
+
+@pytest.mark.parametrize("d,n", [(128, 1200), (128, 100), (64, 900), (32, 500), (16, 300)])
+@pytest.mark.parametrize("cap,scale", [(61.0, None), (100.0, 1.0), (500.0, 3.0)])
+def test_caps_that_need_the_maximum(d, n, cap, scale):
+    c = Long(n, 4, 2, d, "bf16", seed=32, causal=True, cap=cap, scale=scale)
+    c.check_backward(*c.check_forward())
