@@ -26,7 +26,8 @@ extern "C" {
  *                      and  (doc = NULL, or doc_i = doc_j >= 0)
  *   lse_i = log sum_{visible j} exp(s_ij),          A_i = sum_{visible j} exp(s_ij - lse_i) v_j
  * A row that sees nothing (a token of no document: doc < 0) has A_i = +0 and lse_i = -inf; its gradients are +0.
- * Values of keys that a query does not see never reach its results, not even infinities and NaN.
+ * Values of keys that a query does not see never reach its results, not even infinities and NaN.  (Calls on tensors that hold such values
+ * take up to some 13 times as long: results that are not finite are computed again without what they do not see.)
  * The backward is "Drop QKV" on the kept tokens (see sbp_backward_attention): i and j run over the kept tokens of the
  * sample only, lse and A come from the forward over all tokens:
  *   P_ij  = exp(s_ij - lse_i) for visible j, else 0

@@ -14,7 +14,7 @@
 // stays three tiles long in a ring of three; one barrier per tile.
 // Tiles of which the workgroup sees nothing are left out of the list (ranges of positions and documents per tile; any order of the kept
 // tokens is right, ascending order makes it short).  Tiles that are visible altogether come first, in a loop without mask arithmetic.
-// Where a result is not finite, its row is computed again one row at a time (see sbp_lm_attention_fwd.h).
+// Where a result is not finite, its row is computed again without the tokens it does not see (sbp_lm_attention_rows.h).
 // Bound, d = 128 (one wavefront per SIMD): what one wavefront can issue; counted over the busy cycles of a CU, capped, the matrix cores are busy
 // 35 %, the vector units 49 %, the LDS 31 % (a layout without its conflicts: no gain), uncapped 44, 33 and 38 %, at a clock of 2.1 GHz.
 // 16 heads sharing 2, 4096 of 8192 tokens, causal, capped: 330 .. 380 us on the cards seen with the first kernel's 7 and the last one's 5,
@@ -333,17 +333,14 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (D >= 32 || e < 8) fine = fine && lm_finite(acc[q][x][e]);
-  unsigned long long again = __ballot(!fine);
-  again = (again | again >> 32) & 0xffffffffull;
+  const unsigned long long bad = __ballot(!fine);
+  const uint32_t again = (uint32_t)(bad | bad >> 32);
   const float dscale = CAP ? 4.f * a.scale : a.scale;
   uint16_t* out = (uint16_t*)a.out + row0 * ld;
   char* img = smem + wave * (2 * 32 * (2 * D + 16));
   if constexpr (!KEY) {
     attn_store_rows<D>(img, acc[0], dscale, out + h0 * D, ld, first, rows, lane);
-    for (; again; again &= again - 1) {
-      const int q = first + __ffsll((long long)again) - 1;
-      if (q < rows) lm_backward_query<uint16_t>(a, b, h0, q, lane);
-    }
+    if (__builtin_expect(again != 0, 0)) lm_backward_again<uint16_t, D, false>(a, w, b, kv, h0, 1, first, again, lane, nullptr);
   } else {
     float* part = w.part ? w.part + (((long long)(group % w.parts) * a.B + b) * rows * a.hk + kv) * (2 * D) : nullptr;
     if (!part) {
@@ -359,24 +356,7 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
           *reinterpret_cast<float4*>(p + D + 32 * x + 8 * q4) = make_float4(acc[1][x][4 * q4], acc[1][x][4 * q4 + 1], acc[1][x][4 * q4 + 2], acc[1][x][4 * q4 + 3]);
         }
     }
-    for (; again; again &= again - 1) {
-      const int j = first + __ffsll((long long)again) - 1;
-      if (j >= rows) continue;
-      float dk[2], dv[2];
-      lm_backward_key<uint16_t>(a, b, kv, h0, h0 + nh, j, lane, dk, dv);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c = lane + 64 * e;
-        if (c >= D) continue;
-        if (part) {
-          part[(long long)j * (a.hk * 2 * D) + c] = dk[e];
-          part[(long long)j * (a.hk * 2 * D) + D + c] = dv[e];
-        } else {
-          lm_store(out + (long long)j * ld + (a.h + kv) * D + c, dk[e]);
-          lm_store(out + (long long)j * ld + (a.h + a.hk + kv) * D + c, dv[e]);
-        }
-      }
-    }
+    if (__builtin_expect(again != 0, 0)) lm_backward_again<uint16_t, D, true>(a, w, b, kv, h0, nh, first, again, lane, part);
   }
 }
 

@@ -73,14 +73,6 @@ template <int D> struct LmF32 {
   }
 };
 
-// tanh to about a step of fp32, without branches: up to 0.55 an odd polynomial (of least largest error, 2^-29 of the value), beyond it
-// 1 - 2 / (exp(2 |x|) + 1).  (tanhf() takes both of its ways where the lanes differ.)
-__device__ __forceinline__ float lm_tanh(float x) {
-  const float u = x * x, y = fabsf(x);
-  const float near = fmaf(x * u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -0.0062824725f, 0.021077758f), -0.05385386f), 0.13332602f), -0.3333332f), x);
-  const float far = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.f * kLog2e)) + 1.f), 1.f);
-  return y > 0.55f ? copysignf(far, x) : near;
-}
 // the score (natural units) of z = q.k and, capped, the square of its tanh
 template <bool CAP>
 __device__ __forceinline__ float lm_score_f32(const MaskedAttention& a, float inv_cap, float slope, float z, float distance, float* t2) {
@@ -94,7 +86,7 @@ __device__ __forceinline__ float lm_score_f32(const MaskedAttention& a, float in
 }
 
 template <int D, bool CAP>
-__global__ void __launch_bounds__(256) masked_forward_f32_kernel(MaskedAttention a) {
+__global__ void __launch_bounds__(256, D <= 32 ? 3 : D == 64 ? 2 : 1) masked_forward_f32_kernel(MaskedAttention a) {
   using F = LmF32<D>;
   __shared__ __attribute__((aligned(16))) float img[4 * 32 * F::PITCH];
   __shared__ float m_s[4][32], l_s[4][32];
@@ -211,17 +203,14 @@ __global__ void __launch_bounds__(256) masked_forward_f32_kernel(MaskedAttention
     }
     const bool empty = total == 0.f;
     const float f = empty ? 0.f : 1.f / total;
-    if (!(lm_finite(total) && lm_finite(s.x) && lm_finite(s.y) && lm_finite(s.z) && lm_finite(s.w))) atomicOr(&again_s, 1u << row);
+    if (lm_finite(total) && !(lm_finite(s.x) && lm_finite(s.y) && lm_finite(s.z) && lm_finite(s.w))) atomicOr(&again_s, 1u << row);
     if (first + row < n) {
       *reinterpret_cast<float4*>(out + (first + row) * ((long long)a.h * D) + c) = empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(s.x * f, s.y * f, s.z * f, s.w * f);
       if (a.lse_out && c == 0) a.lse_out[((long long)b * n + first + row) * a.h + head] = empty ? -INFINITY : ms + logf(total);
     }
   }
   __syncthreads();
-  for (uint32_t w = again_s; w; w &= w - 1) {                // (see sbp_lm_attention_fwd.h)
-    const int row = __ffs((int)w) - 1;
-    if ((row & 3) == wave && first + row < n) lm_forward_row<float>(a, b, head, first + row, lane);
-  }
+  if (__builtin_expect(wave == 0 && again_s, 0)) lm_forward_again<float, D>(a, b, head, first, again_s, lane);      // (see sbp_lm_attention_fwd.h)
 }
 
 // ---- backward ------------------------------------------------------------------------------------------------------
@@ -349,24 +338,7 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
     }
   }
   __syncthreads();
-  for (uint32_t x = *again_s; x; x &= x - 1) {
-    const int row = __ffs((int)x) - 1, tok = first + row;
-    if ((row & 3) != wave || tok >= rows) continue;
-    if constexpr (!KEY) {
-      lm_backward_query<float>(a, b, h0, tok, lane);
-    } else {
-      float dk[2], dv[2];
-      lm_backward_key<float>(a, b, kv, h0, h0 + nh, tok, lane, dk, dv);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c = lane + 64 * e;
-        if (c >= D) continue;
-        float* o = part ? part + (long long)tok * (a.hk * 2 * D) : out + tok * ld + (a.h + kv) * D;
-        o[c] = dk[e];
-        o[(part ? D : a.hk * D) + c] = dv[e];
-      }
-    }
-  }
+  if (__builtin_expect(wave == 0 && *again_s, 0)) lm_backward_again<float, D, KEY>(a, w, b, kv, h0, nh, first, *again_s, lane, part);
 }
 
 template <int D, bool CAP>

@@ -17,7 +17,7 @@
 // ranges per tile; without, they are a run of tiles.  A wavefront works from the first to the last of them that it sees itself, and
 // masks element by element only where a tile is not visible altogether.
 // A value that is not finite in a row of v whose weight is 0 turns into NaN in the product.  Where the result of a query is not
-// finite, its row is computed again one row at a time, without the keys it does not see.
+// finite, its row is computed again without the keys it does not see (sbp_lm_attention_rows.h).
 // Bound, d = 128: the products of one half against the vector arithmetic of the other, at the clock that the card keeps under them (counted over the
 // busy cycles of a CU, capped: matrix cores 41 %, vector units 64 %, LDS 31 %, 1.95 GHz; uncapped 51, 46, 40 %, 1.9 GHz); 16 heads sharing
 // 2, 8192 tokens, causal, capped: 302 .. 355 us on the cards seen (275 GFLOP counted, 0.8 .. 0.9 PFLOP/s), uncapped 280 (0.98).
@@ -57,8 +57,9 @@ struct LmFwd {
   static constexpr size_t LDS = DOCS + 4 * 4 * kLmTile > OUT ? DOCS + 4 * 4 * kLmTile : OUT;
 };
 
+// (workgroups per CU of 4 wavefronts: what the loops leave room for; without the bias d <= 32 for four)
 template <int D, int NW, int MODE>
-__global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kernel(MaskedAttention a, int nchunks) {
+__global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_PLAIN || MODE == LM_CAP_FIXED) ? 4 : 3) masked_forward_kernel(MaskedAttention a, int nchunks) {
   using L = AttnSwizzled<D>;
   using F = LmFwd<D, NW>;
   constexpr int KS = L::KS, DB = L::DB;
@@ -383,22 +384,20 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : 3) masked_forward_kern
   l += __shfl_xor(l, 32);
   const bool empty = l == 0.f;
   const float f = empty ? 0.f : 1.f / l;
-  bool fine = lm_finite(l);
+  bool fine = true;
 #pragma unroll
   for (int x = 0; x < DB; ++x)
 #pragma unroll
     for (int e = 0; e < 16; ++e)
       if (D >= 32 || e < 8) fine = fine && lm_finite(o[x][e]);
+  fine = fine || !lm_finite(l);                              // (a sum of weights has seen scores alone: this row is NaN as it should be)
   uint16_t* out = (uint16_t*)a.out + (long long)b * n * (a.h * D) + head * D;
   attn_store_rows<D>(smem + wave * (32 * (2 * D + 16)), o, f, out, (long long)a.h * D, first, n, lane);
   if (a.lse_out && u == 0 && mine < n)
     a.lse_out[((long long)b * n + mine) * a.h + head] = empty ? -INFINITY : (m2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-  unsigned long long again = __ballot(!fine);
-  again = (again | again >> 32) & 0xffffffffull;
-  for (; again; again &= again - 1) {
-    const int q = first + __ffsll((long long)again) - 1;
-    if (q < n) lm_forward_row<uint16_t>(a, b, head, q, lane);
-  }
+  const unsigned long long bad = __ballot(!fine);
+  const uint32_t again = (uint32_t)(bad | bad >> 32);
+  if (__builtin_expect(again != 0, 0)) lm_forward_again<uint16_t, D>(a, b, head, first, again, lane);
 }
 
 template <int D, int NW, int MODE>

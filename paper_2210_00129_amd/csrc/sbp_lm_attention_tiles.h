@@ -3,24 +3,9 @@
 #ifndef SBP_LM_ATTENTION_TILES_H_
 #define SBP_LM_ATTENTION_TILES_H_
 
-#include "sbp_attention_tiles.h"
 #include "sbp_lm_attention_rows.h"
 
 namespace sbp {
-
-static constexpr int kLmTile = 64;                         // streamed tokens per tile
-
-static constexpr int kLmChunk = 128;                       // own tokens per workgroup of the backward
-
-// What the first kernel of the backward writes (workspace): npad = rows rounded up to whole tiles.
-struct LmTables {
-  float *l2, *nd;                // [B*h][npad]
-  float* pos;                    // [B][npad], NaN past the last token: no comparison with it is true
-  int32_t* doc;                  // [B][npad]
-  int4* range;                   // [B][npad / 64]: positions, documents (0, 0 without documents) of the tile's tokens
-  float* part;                   // [parts][B*rows][hk][2][D]: dK, dV of the parts of a key / value head
-  int npad, parts, nchunks;
-};
 
 // Positions and documents of some tokens, as ranges: positions p0 .. p1; documents d0 .. d1 of the tokens that belong to one (none:
 // d0 > d1), made wider where others belong to none, so that d0 = d1 means that all of them belong to that one.
@@ -76,8 +61,6 @@ __device__ __forceinline__ void lm_copy4(const void* base, uint32_t off, uint32_
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory");
 }
 __device__ __forceinline__ void lm_copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
-__device__ __forceinline__ bool lm_finite(float v) { return fabsf(v) < INFINITY; }
 
 // Copies of a tile of kLmTile rows of 2 D bytes into an LDS image, shared out over NW wavefronts.
 template <int D, int NW>
