@@ -34,9 +34,9 @@ namespace sbp {
 // Score arithmetic: plain (scale > 0), with the distance bias (any scale), capped with |score| <= cap <= 60 and no bias (weights
 // exp(score) themselves: no maximum is needed, exp(-60) .. exp(60) and their sums stay within fp32), capped otherwise.
 enum LmMode { LM_PLAIN = 0, LM_BIAS = 1, LM_CAP_FIXED = 2, LM_CAP = 3 };
-// (Fixed: the long text 347 us, with the running maximum 419.  A row all of whose scores are near -cap loses what is below 2^-126 e^cap, 1.3e-12
-// for 60, of its values.)
-static constexpr float kLmSlack = 6.f, kLmFixedCap = 60.f;
+// (Fixed, cap 50: the long text 347 us when it was made, with the running maximum 419.  Products of a weight and a value below 2^-126 are lost, so
+// a row whose weights sum to less than kLmFixedSum, all scores below -41, is computed again with its maximum, and no other loses more than 2^-66 of A.)
+static constexpr float kLmSlack = 6.f, kLmFixedCap = 60.f, kLmFixedSum = 0x1p-60f;
 static constexpr int kLmAhead = 6;                         // (the long text uncapped 283 us; 2: 287)
 static constexpr int kLmList = 128;                        // tiles per list (8192 tokens); longer samples take several
 
@@ -391,6 +391,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_
     for (int e = 0; e < 16; ++e)
       if (D >= 32 || e < 8) fine = fine && lm_finite(o[x][e]);
   fine = fine || !lm_finite(l);                              // (a sum of weights has seen scores alone: this row is NaN as it should be)
+  if constexpr (MODE == LM_CAP_FIXED) fine = fine && !(l > 0.f && l < kLmFixedSum);
   uint16_t* out = (uint16_t*)a.out + (long long)b * n * (a.h * D) + head * D;
   attn_store_rows<D>(smem + wave * (32 * (2 * D + 16)), o, f, out, (long long)a.h * D, first, n, lane);
   if (a.lse_out && u == 0 && mine < n)

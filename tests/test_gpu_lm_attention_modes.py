@@ -28,3 +28,14 @@ def test_scales_of_zero_and_below(scale, mods, dtype):
 def test_caps_that_need_the_maximum(d, n, cap, scale):
     c = Long(n, 4, 2, d, "bf16", seed=32, causal=True, cap=cap, scale=scale)
     c.check_backward(*c.check_forward())
+
+
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("cap,size", [(60.0, 1e-13), (60.0, 1e-18), (45.0, 1e-18), (20.0, 1e-18)])
+def test_small_values_of_rows_at_the_lower_cap(d, cap, size):
+    """Every score of a row near -cap and values so small that exp(-cap) of them is below fp32's range."""
+    c = Case(1, 300, 1, 1, d, "bf16", seed=33, causal=True, cap=cap)
+    c.qkv[:, :d] = 40.0
+    c.qkv[:, d:2 * d] = -40.0
+    c.qkv[:, 2 * d:] *= size
+    check_forward(c)
