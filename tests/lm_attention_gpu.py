@@ -57,6 +57,10 @@ class Long:
 
     def check_forward(self):
         A, lse = sbp.forward_attention_masked(self.qkv, **self.kw)
+        self.hold_forward(A, lse)
+        return A, lse
+
+    def hold_forward(self, A, lse):
         pos, terms = torch.arange(self.n, device="cuda"), 2 * self.n * 2.0 ** -24
         for a in range(self.h):
             c = a * self.hk // self.h
@@ -72,15 +76,19 @@ class Long:
             got = lse[:, a].double()
             assert torch.equal(got == -torch.inf, empty)
             assert ((got - l)[~empty].abs() <= 1.01 * (rel + 2.0 ** -22 * (1 + l.abs()))[~empty]).all(), ("lse", a)
-        return A, lse
 
     def check_backward(self, A=None, lse=None):
         """On the kept tokens; A and lse (of all tokens): the forward's unless given."""
         if A is None:
             A, lse = sbp.forward_attention_masked(self.qkv, **self.kw)
+        ins = [t[self.kept].contiguous() for t in (self.qkv, A, self.dA, lse)]
+        out = sbp.backward_attention_masked(*ins, n=self.n, idx=self.idx, **self.kw)
+        self.hold_backward(*ins, out)
+        return out
+
+    def hold_backward(self, qkv, A, dA, lse, out):
+        """The kept tokens' gradients `out` to the definition on these inputs."""
         at, m, share = self.kept, len(self.kept), self.h // self.hk
-        qkv, dA, A, lse = (t[at].contiguous() for t in (self.qkv, self.dA, A, lse))
-        out = sbp.backward_attention_masked(qkv, A, dA, lse, n=self.n, idx=self.idx, **self.kw)
         terms = 2 * m * 2.0 ** -24 * share
         for c in range(self.hk):
             k, v = self.head(qkv, self.h + c), self.head(qkv, self.h + self.hk + c)
@@ -105,4 +113,3 @@ class Long:
                 bv += (P * (self._bf() + delta + terms)).t().contiguous() @ g.abs()
             self._held(self.head(out, self.h + c), dk, bk, ("dk", c))
             self._held(self.head(out, self.h + self.hk + c), dv, bv, ("dv", c))
-        return out
