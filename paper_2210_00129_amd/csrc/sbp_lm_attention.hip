@@ -6,8 +6,8 @@
 
 namespace sbp {
 
-// What the backward's main kernel reads per token (LmTables).  Bound: the read of A and dA (4 x 12 heads of 64, 1024 kept tokens: 12.6 MB, 5.3 us of
-// which most is the launch and one round trip to memory; 16 heads of 128, 4096 tokens: 33.5 MB, 7.3 us);
+// What the backward's main kernel reads per token (LmTables).  Bound: the read of A and dA (4 x 12 heads of 64, 1024 kept tokens: 12.6 MB, 5.4 us of
+// which most is the launch and one round trip to memory; 16 heads of 128, 4096 tokens: 33.5 MB, 8.0 us);
 // all of a wavefront's loads are under way at once.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) masked_prepare_kernel(MaskedAttention a, LmTables w) {
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(256) masked_join_kernel(MaskedAttention a, LmT
 
 // Parts of a key / value head: its query heads follow one another in one workgroup per 128 keys (fp32: 32) unless that leaves fewer
 // workgroups of this kind than CUs (256); then they are dealt to the smallest number of parts that does not, each one more set of fp32
-// dK and dV.  (16 heads of 128 sharing 2, 4096 kept tokens: 4 parts 394 us, 2 parts 567, 8 parts 394 with twice the workspace.)
+// dK and dV.  (16 heads of 128 sharing 2, 4096 kept tokens: 4 parts 331 us, 2 parts 553, 8 parts 334 with twice the workspace.)
 static int masked_parts(int64_t heads, int share, int nchunks) {
   int p = 1;
   while (p < share && heads * p * nchunks < 256) {

@@ -17,9 +17,9 @@
 // Where a result is not finite, its row is computed again without the tokens it does not see (sbp_lm_attention_rows.h).
 // Bound, d = 128 (one wavefront per SIMD): what one wavefront can issue; counted over the busy cycles of a CU, capped, the matrix cores are busy
 // 35 %, the vector units 49 %, the LDS 31 % (a layout without its conflicts: no gain), uncapped 44, 33 and 38 %, at a clock of 2.1 GHz.
-// 16 heads sharing 2, 4096 of 8192 tokens, causal, capped: 330 .. 380 us on the cards seen with the first kernel's 7 and the last one's 5,
-// uncapped 296.  d = 64: vector arithmetic and the chain of a workgroup's tiles; 4 x 12 heads of 64, 1024 of 2048 tokens in documents of
-// 500 on average, biased: 35 .. 41 us (a CU is busy 63 % of it on average); 16 samples of it 121.
+// 16 heads sharing 2, 4096 of 8192 tokens, causal, capped: 330 .. 350 us with the first kernel's 8 and the last one's 7 (up to 380 at lower clocks),
+// uncapped 277.  d = 64: vector arithmetic and the chain of a workgroup's tiles; 4 x 12 heads of 64, 1024 of 2048 tokens in documents of
+// 500 on average, biased: 35 .. 39 us (a CU is busy 63 % of it on average); 16 samples of it 110.
 #ifndef SBP_LM_ATTENTION_BWD_H_
 #define SBP_LM_ATTENTION_BWD_H_
 
@@ -109,7 +109,7 @@ __device__ __forceinline__ void masked_backward_body(char* smem, int* list_s, in
   // half 0 or 1 of its tile), scores of the next one (st, sj).  Operands are read AHEAD
   // products before they are multiplied, the first ones of a turn (and the first rows of its table) at the end of the turn before: a
   // product takes 32 cycles, a read of LDS under way some 150.
-  // (d = 64 with the bias: 4 ahead leave 16 registers in memory, 16 samples of the packed documents 123 us, 2 ahead 120)
+  // (d = 64 with the bias: 4 ahead leave more in memory, 16 samples of the packed documents 115 us, 2 ahead 110)
   constexpr int NP = 2 * DB * NACC, N = NP + 2 * KS, AHEAD = D == 128 ? 8 : D == 64 && !BIAS ? 4 : 2;
   static_assert(AHEAD <= NP && N % AHEAD == 0, "the operands read ahead are products' and keep their places from turn to turn");
   bf16x8_t f[AHEAD];
@@ -365,8 +365,8 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) masked_backward_kernel(
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int list_s[kLmBwdList], count_s[2];
   // Units: the key groups and the query heads of all samples, each for every rank; those of one XCD stay on it where both divide by 8.
-  // d = 128 (one workgroup on a CU): all key units first, the longer kind (the long text 379 us, mixed by rank 391).  Smaller heads (two): mixed,
-  // since a key and a query unit share a CU better than two key units (packed documents 41 us, key units first 44).
+  // d = 128 (one workgroup on a CU): all key units first, the longer kind (the long text 331 us, mixed by rank 348).  Smaller heads (two): mixed,
+  // since a key and a query unit share a CU better than two key units (packed documents 37 us, key units first 41).
   const int nk = a.B * a.hk * w.parts, nq = a.B * a.h, x8 = nk % 8 == 0 && nq % 8 == 0 ? 8 : 1, pk = nk / x8, pq = nq / x8;
   const int x = blockIdx.x % x8, j = blockIdx.x / x8;
   int rank, k;

@@ -20,10 +20,10 @@
 // finite, its row is computed again without the keys it does not see (sbp_lm_attention_rows.h).
 // Bound, d = 128: the products of one half against the vector arithmetic of the other, at the clock that the card keeps under them (counted over the
 // busy cycles of a CU, capped: matrix cores 41 %, vector units 64 %, LDS 31 %, 1.95 GHz; uncapped 51, 46, 40 %, 1.9 GHz); 16 heads sharing
-// 2, 8192 tokens, causal, capped: 302 .. 355 us on the cards seen (275 GFLOP counted, 0.8 .. 0.9 PFLOP/s), uncapped 280 (0.98).
+// 2, 8192 tokens, causal, capped: 295 .. 320 us (275 GFLOP counted, 0.86 .. 0.93 PFLOP/s; up to 355 at lower clocks), uncapped 267 (1.03).
 // d = 64: vector arithmetic, and for short documents the chain of a workgroup's few tiles (1.25 us each with one workgroup on a CU, some 8 us
 // before and after them) and their unequal number (a CU is busy half of the time on average); 4 x 12 heads of 64, 2048 tokens in documents of
-// 500 on average, biased: 33 .. 37 us; without documents and bias 46 us (0.56 PFLOP/s), 16 samples of it 140 (0.73).
+// 500 on average, biased: 33 .. 37 us; without documents and bias 44 us (0.59 PFLOP/s), 16 samples of it 144 (0.72).
 #ifndef SBP_LM_ATTENTION_FWD_H_
 #define SBP_LM_ATTENTION_FWD_H_
 
@@ -34,10 +34,10 @@ namespace sbp {
 // Score arithmetic: plain (scale > 0), with the distance bias (any scale), capped with |score| <= cap <= 60 and no bias (weights
 // exp(score) themselves: no maximum is needed, exp(-60) .. exp(60) and their sums stay within fp32), capped otherwise.
 enum LmMode { LM_PLAIN = 0, LM_BIAS = 1, LM_CAP_FIXED = 2, LM_CAP = 3 };
-// (Fixed, cap 50: the long text 347 us when it was made, with the running maximum 419.  Products of a weight and a value below 2^-126 are lost, so
+// (Fixed, cap 50: the long text 310 us, with the running maximum 368.  Products of a weight and a value below 2^-126 are lost, so
 // a row whose weights sum to less than kLmFixedSum, all scores below -41, is computed again with its maximum, and no other loses more than 2^-66 of A.)
 static constexpr float kLmSlack = 6.f, kLmFixedCap = 60.f, kLmFixedSum = 0x1p-60f;
-static constexpr int kLmAhead = 6;                         // (the long text uncapped 283 us; 2: 287)
+static constexpr int kLmAhead = 6;                         // (the long text uncapped 267 us; 2: 269)
 static constexpr int kLmList = 128;                        // tiles per list (8192 tokens); longer samples take several
 
 // max(a, b, c); of the numbers where some are NaN.  (fmaxf() first makes every operand that the compiler does not know to be a quiet
@@ -174,8 +174,8 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_
         common[1] = -slope2 * (relf - 32.f);
       }
       if constexpr (CAP) {
-        // cap tanh(z / cap) by one exponential and a reciprocal (a polynomial for small arguments has more steps than these: the long text
-        // 372 us instead of 313)
+        // cap tanh(z / cap) by one exponential and a reciprocal (a polynomial for small arguments has more steps than these: 19 % more time
+        // for the long text)
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -418,9 +418,10 @@ static void launch_masked_forward_mode(const MaskedAttention& a, hipStream_t s) 
 }
 template <int D>
 void launch_masked_forward_bf16(const MaskedAttention& a, hipStream_t s) {
-  // Pairs of wavefronts half a stage apart pay where the products of a stage are many (d = 128: the long text 314 us, with 4 wavefronts
-  // 398) and there is more than one workgroup of 4 to a head; for smaller d the meetings cost more than they hide (4 x 12 heads of 64,
-  // 2048 packed tokens: 62 us with 4 wavefronts, 80 with 8; 16 samples of them 163 and 218).
+  // Pairs of wavefronts half a stage apart pay where the products of a stage are many (d = 128: the long text 310 us, with 4 wavefronts
+  // 335, uncapped 267 and 294; with the running maximum and the cap, whose arithmetic is the most, 367 and 363) and there is more than one workgroup
+  // of 4 to a head; for smaller d the meetings cost more than they hide (4 x 12 heads of 64, 2048 packed tokens: 35 us with 4 wavefronts, 50
+  // with 8; 16 samples of them 94 and 159).
   if constexpr (D == 128) {
     if (a.n > 128) return launch_masked_forward_mode<D, 8>(a, s);
   }

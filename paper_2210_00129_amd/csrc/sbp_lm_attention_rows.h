@@ -58,8 +58,9 @@ __device__ __forceinline__ int lm_prefix(const MaskedAttention& a, int b) { retu
 __device__ __forceinline__ bool lm_visible(const MaskedAttention& a, int prefix, int pi, int di, int pj, int dj) {
   return (!a.causal || pj <= pi || pj < prefix) && di == dj && di >= 0;
 }
-// tanh to about a step of fp32, without branches: up to 0.55 an odd polynomial (of least largest error, 2^-29 of the value), beyond it
-// 1 - 2 / (exp(2 |x|) + 1).  (tanhf() takes both of its ways where the lanes differ.)
+// tanh to about a step of fp32, without branches: up to 0.55, about (ln 3) / 2, an odd polynomial (fitted for the least largest error, 2^-29 of the
+// value), beyond it 1 - 2 / (exp(2 |x|) + 1); the split and the upper branch as in Cody and Waite, Software Manual for the Elementary
+// Functions.  (tanhf() takes both of its ways where the lanes differ.)
 __device__ __forceinline__ float lm_tanh(float x) {
   const float u = x * x, y = fabsf(x);
   const float near = fmaf(x * u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -0.0062824725f, 0.021077758f), -0.05385386f), 0.13332602f), -0.3333332f), x);

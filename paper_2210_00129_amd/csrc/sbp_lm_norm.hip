@@ -1,6 +1,7 @@
 // The step between two blocks (sbp_lm.h): norm after a block, gate, residual sum, norm before the next block; and its backward
 // on the kept rows.
-// A team of TS threads owns a row and keeps it in registers (E channels per thread, 8 up to 8192 channels), so that every tensor is read once and
+// A team of TS threads owns a row and keeps it in registers (E channels per thread: 8 up to 8192 channels, 16 beyond; in the backward 16 from 4097 on
+// but for single channels without the sums of shifts), so that every tensor is read once and
 // written once; the row's sums go over the wavefront and, for teams of several wavefronts, through LDS with one barrier per round.
 // Bound: HBM.  16384 x 4096, bf16, both norms: forward 106 us for 537 MB (5.1 TB/s, what a copy of 1 GiB reaches); backward with half of
 // the rows kept 122 us, 7 of them the sums of the partial sums (537 MB, 4.6 TB/s without them).
