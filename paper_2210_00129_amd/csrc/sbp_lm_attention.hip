@@ -6,8 +6,8 @@
 
 namespace sbp {
 
-// What the backward's main kernel reads per token (LmTables).  Bound: the read of A and dA (4 x 12 heads of 64, 1024 kept tokens: 12.6 MB, 5.4 us of
-// which most is the launch and one round trip to memory; 16 heads of 128, 4096 tokens: 33.5 MB, 8.0 us);
+// What the backward's main kernel reads per token (LmTables).  Bound: the read of A and dA (4 x 12 heads of 64, 1024 kept tokens: 12.6 MB, 4.8 us of
+// which most is the launch and one round trip to memory; 16 heads of 128, 4096 tokens: 33.5 MB, 8.3 us);
 // all of a wavefront's loads are under way at once.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) masked_prepare_kernel(MaskedAttention a, LmTables w) {
