@@ -5,7 +5,10 @@
 //   S^T = K Q^T: rows j, column i = lane (v_mfma_f32_32x32x16_bf16, layouts at sbp_attention.hip).  A query's scores of a block of 32
 //   keys are 16 registers in each of lanes i and i + 32, so its maximum and sum need one exchange between the halves, and P^T is,
 //   packed to bf16, the B operand of O^T += V^T P^T as it is; V^T comes out of LDS with transposing reads.
-// P is rounded to bf16 (2^-8 of the weight) because the matrix cores multiply bf16; its sum l is taken before the rounding.
+// P is rounded to bf16 (2^-8 of the weight) because the matrix cores multiply bf16; its sum l is taken before the rounding.  Where no maximum is
+// taken out (LM_CAP_FIXED), A is divided by the sum of the rounded weights instead: a row's largest weight is then not 1, and what its rounding
+// does to sum and products alike cancels (one key: A = v as it is; error against 64 bits, documents of 9 tokens on average 0.0021 -> 0.0017,
+// 500 tokens 0.0023 -> 0.0021; the long text 308 -> 314 us, 4 x 12 heads of 64 sharing 4, 2048 tokens 55 -> 56).
 // The running maximum moves only when a block's maximum is more than kLmSlack above it (weights up to 2^kLmSlack instead of 1: no loss
 // in a floating format), so that the accumulators are rescaled rarely.
 // A stage of the loop has a product part M(t) = {O += V(t-1) P(t-1); S(t) = K(t) Q} and an arithmetic part A(t) = softmax of S(t), in
@@ -37,6 +40,7 @@ enum LmMode { LM_PLAIN = 0, LM_BIAS = 1, LM_CAP_FIXED = 2, LM_CAP = 3 };
 // (Fixed, cap 50: the long text 310 us, with the running maximum 368.  Products of a weight and a value below 2^-126 are lost, so
 // a row whose weights sum to less than kLmFixedSum, all scores below -41, is computed again with its maximum, and no other loses more than 2^-66 of A.)
 static constexpr float kLmSlack = 6.f, kLmFixedCap = 60.f, kLmFixedSum = 0x1p-60f;
+static constexpr uint32_t kLmOnes = 0x3f803f80u;           // two ones
 static constexpr int kLmAhead = 6;                         // (the long text uncapped 267 us; 2: 269)
 static constexpr int kLmList = 128;                        // tiles per list (8192 tokens); longer samples take several
 
@@ -131,6 +135,7 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[x][e] = 0.f;
   float m2 = MODE == LM_CAP_FIXED ? 0.f : -INFINITY, l = 0.f;      // the maximum in units of log2, the half's share of the sum
+  float lr[4] = {0.f, 0.f, 0.f, 0.f};                       // LM_CAP_FIXED: the same of the rounded weights (four sums: one waits for itself)
 
   f32x16_t sc[2];                                            // scores of the tile's two blocks of 32 keys
   bf16x8_t pw[2][2];                                         // their weights
@@ -258,7 +263,16 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_
         l += sc[y][e];
       }
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) pw[y][ks] = pack8(sc[y], ks);
+      for (int ks = 0; ks < 2; ++ks) {
+        pw[y][ks] = pack8(sc[y], ks);
+        if constexpr (MODE == LM_CAP_FIXED) {
+          const uint4 w = __builtin_bit_cast(uint4, pw[y][ks]);
+          lr[0] = attn_dot2(w.x, kLmOnes, lr[0]);
+          lr[1] = attn_dot2(w.y, kLmOnes, lr[1]);
+          lr[2] = attn_dot2(w.z, kLmOnes, lr[2]);
+          lr[3] = attn_dot2(w.w, kLmOnes, lr[3]);
+        }
+      }
     }
   };
 
@@ -383,7 +397,12 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_
   if (!busy) return;
   l += __shfl_xor(l, 32);
   const bool empty = l == 0.f;
-  const float f = empty ? 0.f : 1.f / l;
+  float total = l;
+  if constexpr (MODE == LM_CAP_FIXED) {
+    total = (lr[0] + lr[1]) + (lr[2] + lr[3]);
+    total += __shfl_xor(total, 32);
+  }
+  const float f = empty ? 0.f : 1.f / total;
   bool fine = true;
 #pragma unroll
   for (int x = 0; x < DB; ++x)

@@ -2,6 +2,7 @@
 those whose weights need no maximum."""
 import numpy as np
 import pytest
+import torch
 
 from lm_attention_gpu import Long
 from lm_util import Case, check_backward, check_forward
@@ -39,3 +40,16 @@ def test_small_values_of_rows_at_the_lower_cap(d, cap, size):
     c.qkv[:, d:2 * d] = -40.0
     c.qkv[:, 2 * d:] *= size
     check_forward(c)
+
+
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("mods", [dict(cap=20.0), dict(cap=60.0), dict(), dict(cap=80.0), dict(slopes=True)])
+def test_a_token_that_sees_itself_alone_has_its_own_value(d, mods):
+    """The rounding of the only weight must not reach the result: documents of one token (and a causal text's first)."""
+    n = 200
+    c = Case(2, n, 2, 1, d, "bf16", seed=34, causal=True, doc=np.stack([np.arange(n), np.arange(n) // 2]), **mods)
+    A, _ = check_forward(c)
+    v = c.qkv.view(2, n, 4, d)[:, :, 3]
+    got = A.cpu().view(2, n, 2, d)
+    for a in range(2):
+        assert torch.equal(got[0, :, a], v[0]) and torch.equal(got[1, ::2, a], v[1, ::2])
