@@ -1,5 +1,6 @@
 // C ABI of the language-model steps (sbp_lm.h): host-side validation, then kernel launches.  Every argument check runs before
 // the first HIP call, so that error paths need no device.
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 
@@ -67,6 +68,7 @@ static MaskedAttention masked_args(const sbp_attention_desc& d, int rows) {
   a.slopes = d.slopes; a.doc = d.doc; a.prefix = d.prefix;
   a.B = d.B; a.n = d.n; a.rows = rows; a.h = d.h; a.hk = d.h_kv; a.d = d.d; a.causal = d.causal;
   a.scale = d.scale; a.cap = d.cap;
+  a.per_cap = d.cap > 0.f ? std::min(std::max(d.scale / d.cap, -1e38f), 1e38f) : 0.f;
   return a;
 }
 

@@ -75,10 +75,10 @@ template <int D> struct LmF32 {
 
 // the score (natural units) of z = q.k and, capped, the square of its tanh
 template <bool CAP>
-__device__ __forceinline__ float lm_score_f32(const MaskedAttention& a, float inv_cap, float slope, float z, float distance, float* t2) {
+__device__ __forceinline__ float lm_score_f32(const MaskedAttention& a, float slope, float z, float distance, float* t2) {
   float s = a.scale * z;
   if constexpr (CAP) {
-    const float t = lm_tanh(s * inv_cap);
+    const float t = lm_tanh(z * a.per_cap);
     *t2 = t * t;
     s = a.cap * t;
   }
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(256, D <= 32 ? 3 : D == 64 ? 2 : 1) masked_for
   const bool docs = a.doc != nullptr;
   const int32_t* doc = docs ? a.doc + (long long)b * n : nullptr;
   const int prefix = lm_prefix(a, b), di = docs ? doc[own] : 0;
-  const float slope = a.slopes ? a.slopes[head] : 0.f, inv_cap = CAP ? 1.f / a.cap : 0.f;
+  const float slope = a.slopes ? a.slopes[head] : 0.f;
   LmRange wq{first, min(first + 31, n - 1), 0, 0};
   if (docs) {
     LmDocs r;
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(256, D <= 32 ? 3 : D == 64 ? 2 : 1) masked_for
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       float unused;
-      s[e] = lm_score_f32<CAP>(a, inv_cap, slope, s[e], fabsf((float)(rel - (8 * (e >> 2) + (e & 3)))), &unused);
+      s[e] = lm_score_f32<CAP>(a, slope, s[e], fabsf((float)(rel - (8 * (e >> 2) + (e & 3)))), &unused);
     }
     if (cls != 2 || j0 + 31 >= n) {
       int lim = n - j0 - 4 * u;
@@ -253,7 +253,6 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[q][x][e] = 0.f;
   if (t == 0) *again_s = 0;
-  const float inv_cap = CAP ? 1.f / a.cap : 0.f;
   const int4* ranges = w.range + (long long)b * tiles;
   const int4 mr4 = ranges[blk >> 1];
   const LmRange mr{mr4.x, mr4.y, mr4.z, mr4.w};
@@ -292,7 +291,7 @@ __device__ __forceinline__ void masked_backward_f32_body(float* img, uint32_t* a
     for (int e = 0; e < 16; ++e) {
       const int q4 = e >> 2, k = e & 3;
       float t2 = 0.f;
-      const float v = lm_score_f32<CAP>(a, inv_cap, slope, s[e], fabsf(tp[q4][k] - own_pos), &t2);
+      const float v = lm_score_f32<CAP>(a, slope, s[e], fabsf(tp[q4][k] - own_pos), &t2);
       float p = expf(v - (KEY ? tl[q4][k] : own_l)), m = p * (dp[e] + (KEY ? tn[q4][k] : own_nd)) * a.scale;
       if constexpr (CAP) m *= 1.f - t2;
       if (masked) {

@@ -122,7 +122,9 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_
   const float slope2 = BIAS && a.slopes ? a.slopes[head] * kLog2e : 0.f;
   float c2 = a.scale * kLog2e;
   if constexpr (BIAS) asm("" : "+v"(c2));                    // (a fused product reads one scalar register: the bias)
-  const float cap2 = a.cap * kLog2e, ct = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f;
+  const float cap2 = a.cap * kLog2e;
+  float ct = 2.f * kLog2e * a.per_cap;
+  if constexpr (CAP) asm("" : "+v"(ct));
   float ahead[BIAS ? 16 : 1];                                // bias of a block's keys relative to the lane's first one (wave-uniform: scalar registers)
   if constexpr (BIAS)
 #pragma unroll

@@ -71,7 +71,7 @@ __device__ __forceinline__ float lm_tanh(float x) {
 __device__ __forceinline__ float lm_score(const MaskedAttention& a, float slope, float z, float distance, float* t) {
   float s = a.scale * z;
   *t = 0.f;
-  if (a.cap > 0.f) { *t = lm_tanh(s / a.cap); s = a.cap * *t; }
+  if (a.cap > 0.f) { *t = lm_tanh(z * a.per_cap); s = a.cap * *t; }
   return slope == 0.f ? s : s - slope * distance;
 }
 __device__ __forceinline__ bool lm_finite(float v) { return fabsf(v) < INFINITY; }

@@ -20,6 +20,7 @@ struct MaskedAttention {
   float* lse_out;
   int B, n, rows, h, hk, d, causal;
   float scale, cap;
+  float per_cap;                 // scale / cap, the factor of q.k under the tanh: finite for the smallest caps too, where 0 times an infinity would be no score
 };
 struct MaskedAttentionPlan {     // workspace of the backward
   int    npad, nchunks;          // kept tokens per sample in whole tiles; chunks of own tokens per workgroup

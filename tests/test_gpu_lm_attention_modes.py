@@ -53,3 +53,15 @@ def test_a_token_that_sees_itself_alone_has_its_own_value(d, mods):
     got = A.cpu().view(2, n, 2, d)
     for a in range(2):
         assert torch.equal(got[0, :, a], v[0]) and torch.equal(got[1, ::2, a], v[1, ::2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cap", [1e-44, 1e-39, 1e-30, 1e-6])
+@pytest.mark.parametrize("scale", [None, 0.0, -1e6])
+@pytest.mark.parametrize("n,d", [(20, 64), (150, 32), (150, 128)])
+def test_smallest_caps(dtype, cap, scale, n, d):
+    """scale / cap beyond fp32: a key whose product with the query is 0 has a score of 0."""
+    c = Case(1, n, 2, 1, d, dtype, seed=35, causal=True, cap=cap, scale=scale)
+    c.qkv[::3, :2 * d] = 0.0
+    check_forward(c)
+    check_backward(c)
