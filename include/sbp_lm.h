@@ -60,8 +60,8 @@ typedef struct sbp_attention_desc {
  *   lse  device, out, [B*n, h] fp32, natural logarithm; or NULL
  * qkv and A 16-byte aligned, A not qkv.  Sums and the softmax statistics are fp32.  In bf16 the weights are rounded to bf16 before the
  * second product: exp(s - a running maximum), or, with 0 < cap <= 60 and no slopes, exp(s) itself, where the row's largest weight is rounded
- * as well (A is divided by the sum of the rounded weights then) and what adds less than 2^-66 to an element of A may be lost; and tanh is good
- * to a few steps of fp32 of 1, so that lse is off by up to 2^-22 cap.  Deterministic.
+ * as well (A is divided by the sum of the rounded weights then) and what adds less than 2^-66 to an element of A may be lost; and beyond 32 tokens
+ * tanh is good to a few steps of fp32 of 1, so that lse is off by up to 2^-22 cap.  Deterministic.
  */
 int32_t sbp_forward_attention_masked(const sbp_attention_desc* desc, const void* qkv, int32_t dtype, void* A, float* lse,
                                      void* stream);

@@ -35,8 +35,12 @@
 namespace sbp {
 
 // Score arithmetic: plain (scale > 0), with the distance bias (any scale), capped with |score| <= cap <= 60 and no bias (weights
-// exp(score) themselves: no maximum is needed, exp(-60) .. exp(60) and their sums stay within fp32), capped otherwise.
-enum LmMode { LM_PLAIN = 0, LM_BIAS = 1, LM_CAP_FIXED = 2, LM_CAP = 3 };
+// exp(score) themselves: no maximum is needed, exp(-60) .. exp(60) and their sums stay within fp32), capped otherwise; short samples, capped in any
+// way: with tanh right to a step of fp32 of the value, where the others' is right to some 2^-22 of the cap.  That error averages out in the lse of
+// many keys, not of few (samples of 1 .. 26 tokens, cap 50: lse off by 1 .. 3e-6 of its size, so below 1e-7).  It takes a fifth more time where many
+// such samples fill the card (400 samples of 32 tokens, 8 heads of 64: 25 -> 30 us), 0.3 us for one.
+enum LmMode { LM_PLAIN = 0, LM_BIAS = 1, LM_CAP_FIXED = 2, LM_CAP = 3, LM_CAP_SHORT = 4 };
+static constexpr int kLmShort = 32;                        // tokens: one block of keys
 // (Fixed, cap 50: the long text 310 us, with the running maximum 368.  Products of a weight and a value below 2^-126 are lost, so
 // a row whose weights sum to less than kLmFixedSum, all scores below -41, is computed again with its maximum, and no other loses more than 2^-66 of A.)
 static constexpr float kLmSlack = 6.f, kLmFixedCap = 60.f, kLmFixedSum = 0x1p-60f;
@@ -67,7 +71,8 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_
   using L = AttnSwizzled<D>;
   using F = LmFwd<D, NW>;
   constexpr int KS = L::KS, DB = L::DB;
-  constexpr bool PAIR = NW == 8, CAP = MODE == LM_CAP || MODE == LM_CAP_FIXED, BIAS = MODE == LM_CAP || MODE == LM_BIAS;
+  constexpr bool PAIR = NW == 8, CAP = MODE == LM_CAP || MODE == LM_CAP_FIXED || MODE == LM_CAP_SHORT,
+                 BIAS = MODE == LM_CAP || MODE == LM_CAP_SHORT || MODE == LM_BIAS;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int4 list_s[kLmList];                           // a tile to look at, the documents in it
   __shared__ int range_s[2 * NW + 1];
@@ -180,7 +185,13 @@ __global__ void __launch_bounds__(64 * NW, D == 128 ? 2 : D < 64 && (MODE == LM_
         common[0] = -slope2 * relf;
         common[1] = -slope2 * (relf - 32.f);
       }
-      if constexpr (CAP) {
+      if constexpr (MODE == LM_CAP_SHORT) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          sc[0][e] = cap2 * lm_tanh(sc[0][e] * a.per_cap);
+          sc[1][e] = -INFINITY;                              // (one tile, whose second block is past the end)
+        }
+      } else if constexpr (CAP) {
         // cap tanh(z / cap) by one exponential and a reciprocal (a polynomial for small arguments has more steps than these: 19 % more time
         // for the long text)
 #pragma unroll
@@ -439,6 +450,7 @@ static void launch_masked_forward_mode(const MaskedAttention& a, hipStream_t s) 
 }
 template <int D>
 void launch_masked_forward_bf16(const MaskedAttention& a, hipStream_t s) {
+  if (a.cap > 0.f && a.n <= kLmShort) return launch_masked_forward<D, 4, LM_CAP_SHORT>(a, s);
   // Pairs of wavefronts half a stage apart pay where the products of a stage are many (d = 128: the long text 310 us, with 4 wavefronts
   // 335, uncapped 267 and 294; with the running maximum and the cap, whose arithmetic is the most, 367 and 363) and there is more than one workgroup
   // of 4 to a head; for smaller d the meetings cost more than they hide (4 x 12 heads of 64, 2048 packed tokens: 35 us with 4 wavefronts, 50

@@ -65,3 +65,24 @@ def test_smallest_caps(dtype, cap, scale, n, d):
     c.qkv[::3, :2 * d] = 0.0
     check_forward(c)
     check_backward(c)
+
+
+@pytest.mark.parametrize("n", [1, 2, 7, 26, 32, 33])
+@pytest.mark.parametrize("mods", [dict(), dict(slopes=True), dict(causal=True)])
+@pytest.mark.parametrize("cap", [20.0, 50.0, 500.0])
+def test_lse_of_few_keys_is_right_to_fp32(n, mods, cap):
+    """bf16, capped: the scores' error, 2^-22 of the cap where tanh is taken from an exponential, does not average out over few keys.  Up to 32
+    tokens lse is held to the steps of fp32 of its own size: z's products and sums, ten steps for tanh, bias and exponentials."""
+    d = 64
+    c = Long(n, 2, 2, d, "bf16", seed=36, cap=cap, **mods)
+    _, lse = c.check_forward()
+    pos = torch.arange(n, device="cuda")
+    for a in range(2):
+        q, k = c.head(c.qkv, a), c.head(c.qkv, 2 + a)
+        s, see, _, _ = c.pairs(q, k, a, pos)
+        z = (q.abs() @ k.abs().t().contiguous()) * c.scale
+        far = 0.0 if c.slopes is None else float(c.slopes[a]) * (pos[None] - pos[:, None]).abs()
+        step = 2.0 ** -24 * ((d + 8) * z + 10 * (s.abs() + far) + 10)
+        want = torch.logsumexp(torch.where(see, s, -torch.inf), 1)
+        bound = torch.where(see, step, 0.0).amax(1) + 2.0 ** -24 * (n + 8 + 4 * want.abs())
+        assert n > 32 or ((lse[:, a].double() - want).abs() <= 1.01 * bound).all()
