@@ -22,8 +22,8 @@
 // A value that is not finite in a row of v whose weight is 0 turns into NaN in the product.  Where the result of a query is not
 // finite, its row is computed again without the keys it does not see (sbp_lm_attention_rows.h).
 // Bound, d = 128: the products of one half against the vector arithmetic of the other, at the clock that the card keeps under them (counted over the
-// busy cycles of a CU, capped: matrix cores 41 %, vector units 64 %, LDS 31 %, 1.95 GHz; uncapped 51, 46, 40 %, 1.9 GHz); 16 heads sharing
-// 2, 8192 tokens, causal, capped: 295 .. 320 us (275 GFLOP counted, 0.86 .. 0.93 PFLOP/s; up to 355 at lower clocks), uncapped 267 (1.03).
+// busy cycles of a CU, capped: matrix cores 40 %, vector units 64 %, LDS 31 %, 1.9 GHz; uncapped 50, 45, 39 %, 1.95 GHz); 16 heads sharing
+// 2, 8192 tokens, causal, capped: 300 .. 325 us (275 GFLOP counted, 0.85 .. 0.92 PFLOP/s; up to 355 at lower clocks), uncapped 267 (1.03).
 // d = 64: vector arithmetic, and for short documents the chain of a workgroup's few tiles (1.25 us each with one workgroup on a CU, some 8 us
 // before and after them) and their unequal number (a CU is busy half of the time on average); 4 x 12 heads of 64, 2048 tokens in documents of
 // 500 on average, biased: 33 .. 37 us; without documents and bias 44 us (0.59 PFLOP/s), 16 samples of it 144 (0.72).
